@@ -16,8 +16,14 @@ LIB_PATH = os.path.join(LIB_DIR, "libspmm_cdna4.so")
 TORCH_EXT_SOURCE = "spmm_torch.cpp"
 TORCH_EXT_PATH = os.path.join(LIB_DIR, "_spmm_torch.so")
 
-SOURCES = ["spmm_kernels.hip", "spmm_tiles.hip", "spmm_strips.hip", "spmm_plan.cpp", "spmm_api.cpp"]
-HEADERS = ["spmm_format.h", "spmm_kernels.h", "spmm_plan.h", "spmm_tiles.h", "spmm_strips.h", "spmm_strips_build.h", "spmm_upload.h", "spmm_launch.h", "spmm_places.h"]
+# the operators beside the product (include/spmm_layers.h) and their tensor-level entries
+LAYERS_EXT_SOURCE = os.path.join("layers", "layers_torch.cpp")
+LAYERS_EXT_PATH = os.path.join(LIB_DIR, "_spmm_layers.so")
+
+SOURCES = ["spmm_kernels.hip", "spmm_tiles.hip", "spmm_strips.hip", "spmm_plan.cpp", "spmm_api.cpp",
+           "layers/quant.hip", "layers/rows.hip", "layers/layers_api.cpp"]
+HEADERS = ["spmm_format.h", "spmm_kernels.h", "spmm_plan.h", "spmm_tiles.h", "spmm_strips.h", "spmm_strips_build.h", "spmm_upload.h", "spmm_launch.h", "spmm_places.h",
+           "layers/layers.h", "layers/elements.h"]
 
 
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
@@ -31,11 +37,12 @@ def _hipcc():
 
 
 def is_stale():
-    if not os.path.exists(LIB_PATH) or not os.path.exists(TORCH_EXT_PATH):
+    built = (LIB_PATH, TORCH_EXT_PATH, LAYERS_EXT_PATH)
+    if not all(map(os.path.exists, built)):
         return True
-    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(TORCH_EXT_PATH))
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + [TORCH_EXT_SOURCE]]
-    deps.append(os.path.join(os.path.dirname(HERE), "include", "spmm.h"))
+    t = min(map(os.path.getmtime, built))
+    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + [TORCH_EXT_SOURCE, LAYERS_EXT_SOURCE]]
+    deps += [os.path.join(os.path.dirname(HERE), "include", f) for f in ("spmm.h", "spmm_layers.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -134,7 +141,7 @@ def build(verbose=False):
               "-I", CSRC, "-I", os.path.join(ROCM, "include"), "-D__HIP_PLATFORM_AMD__=1"]
     objects = []
     for s in SOURCES:
-        obj = os.path.join(obj_dir, os.path.splitext(s)[0] + ".o")
+        obj = os.path.join(obj_dir, os.path.splitext(s)[0].replace("/", "_") + ".o")
         if s.endswith(".hip"):
             cmd = [hipcc, "--offload-arch=gfx950",
                    # packed-fp32 forms are kept out of the generated code on purpose
@@ -161,11 +168,12 @@ def build(verbose=False):
     _run([hipcc, "-shared", "-fPIC"] + objects +
          ["-L", os.path.join(ROCM, "lib"), "-lamdhip64", "-pthread", "-o", LIB_PATH], verbose)
     build_torch_extension(verbose)
+    build_torch_extension(verbose, LAYERS_EXT_SOURCE, LAYERS_EXT_PATH)
     return LIB_PATH
 
 
-def build_torch_extension(verbose=False):
-    """Compile the tensor-level entry (host code: plain C++ against torch's headers), linked
+def build_torch_extension(verbose=False, source=TORCH_EXT_SOURCE, path=TORCH_EXT_PATH):
+    """Compile a tensor-level entry (host code: plain C++ against torch's headers), linked
     to the library beside it.  torch's own copy of the HIP runtime is the one in the process
     (see binding.load), so no runtime is named here."""
     import sysconfig
@@ -175,11 +183,11 @@ def build_torch_extension(verbose=False):
           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
           "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-isystem", os.path.join(ROCM, "include"),
-          os.path.join(CSRC, TORCH_EXT_SOURCE), "-o", TORCH_EXT_PATH,
+          os.path.join(CSRC, source), "-o", path,
           "-L", LIB_DIR, "-lspmm_cdna4", "-Wl,-rpath,$ORIGIN",
           "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip", "-Wl,-rpath," + os.path.join(root, "lib")],
          verbose)
-    return TORCH_EXT_PATH
+    return path
 
 
 if __name__ == "__main__":

@@ -1,0 +1,383 @@
+// C ABI of the operators beside the sparse product (include/spmm_layers.h): the checks of arguments, the layout and
+// upload of 4-bit weights, their life cycle.
+#include "../../../include/spmm_layers.h"
+
+#include <hip/hip_runtime_api.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <exception>
+#include <memory>
+#include <new>
+#include <thread>
+#include <vector>
+
+#include "layers.h"
+
+using namespace layers;
+
+struct spmm_quant {
+    quant_matrix w = {};
+    int device = -1;
+    char *memory = nullptr;
+    int64_t bytes = 0;
+    ~spmm_quant()
+    {
+        if (memory) (void)hipFree(memory);
+    }
+};
+
+namespace {
+
+constexpr int64_t MOST_EXTENT = INT32_MAX;
+// a launch has less than 2^32 threads along an axis: 32 for a row of weights, 2 for a column
+constexpr int64_t MOST_ROWS = (int64_t)1 << 26, MOST_COLS = (int64_t)1 << 30;
+
+int64_t up_to(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
+int64_t parts_of(int64_t n, int64_t part) { return n / part + (n % part != 0); }
+
+spmm_status_t status_of(hipError_t e)
+{
+    if (e == hipSuccess) return SPMM_OK;
+    (void)hipGetLastError();
+    return e == hipErrorOutOfMemory ? SPMM_ERR_ALLOC : SPMM_ERR_HIP;
+}
+
+int64_t size_of(int32_t type) { return type == SPMM_F32 ? 4 : type == SPMM_I8 ? 1 : 2; }
+
+// A tensor's memory and order; SPMM_ERR_INVALID_ARG for what the header rules out.
+spmm_status_t seen(const spmm_tensor_t &t, int64_t features, int64_t tokens, tensor *out)
+{
+    if (t.type < SPMM_F32 || t.type > SPMM_I8 || !t.data || (uintptr_t)t.data % (uintptr_t)size_of(t.type) != 0) return SPMM_ERR_INVALID_ARG;
+    // (an extent of one element leaves the order to the other stride)
+    const bool by_feature = tokens == 1 || t.token_stride == 1, by_token = features == 1 || t.feature_stride == 1;
+    if (by_token && (tokens == 1 || t.token_stride >= features)) *out = {static_cast<char *>(t.data), tokens == 1 ? features : t.token_stride, t.type, true};
+    else if (by_feature && (features == 1 || t.feature_stride >= tokens)) *out = {static_cast<char *>(t.data), features == 1 ? tokens : t.feature_stride, t.type, false};
+    else return SPMM_ERR_INVALID_ARG;
+    // offsets in bytes stay inside 63 bits
+    const int64_t rows = out->by_token ? tokens : features;
+    return out->ld > INT64_MAX / 8 / rows ? SPMM_ERR_INVALID_ARG : SPMM_OK;
+}
+
+struct span {
+    const char *begin, *end;
+};
+
+span span_of(const tensor &t, int64_t features, int64_t tokens)
+{
+    if (!t.data) return {nullptr, nullptr};
+    const int64_t rows = t.by_token ? tokens : features, row = t.by_token ? features : tokens;
+    return {t.data, t.data + ((rows - 1) * t.ld + row) * size_of(t.type)};
+}
+
+bool meet(const span &a, const span &b) { return a.begin && b.begin && a.begin < b.end && b.begin < a.end; }
+
+bool same(const tensor &a, const tensor &b) { return a.data == b.data && a.ld == b.ld && a.by_token == b.by_token; }
+
+// One order for two tensors that share it: where one of them has a single row or column, the other's.  False where they differ.
+bool one_order(tensor *a, const tensor &b, int64_t features, int64_t tokens)
+{
+    if (a->by_token == b.by_token) return true;
+    if (tokens == 1 && a->by_token && a->ld == features) {  // a column without gaps: also features of one token
+        *a = {a->data, 1, a->type, false};
+        return true;
+    }
+    if (features == 1 && !a->by_token && a->ld == tokens) {
+        *a = {a->data, 1, a->type, true};
+        return true;
+    }
+    return false;
+}
+
+// Codes and scales of the tiles [t0, t1) (layers.h).
+void lay_out(const quant_matrix &w, int64_t t0, int64_t t1, const uint8_t *codes, const float *scales, const uint8_t *zeros, uint32_t *out_codes, float *out_scales,
+             uint8_t *out_zeros)
+{
+    const int64_t row_bytes = parts_of(w.K, 2);
+    // the word of eight codes, four bytes as the caller has them (nibble i: column i), in the order of NIBBLE_COLUMN
+    auto ordered = [](uint32_t v) {
+        uint32_t o = 0;
+        for (int i = 0; i < 8; ++i) o |= ((v >> (4 * NIBBLE_COLUMN[i])) & 15u) << (4 * i);
+        return o;
+    };
+    for (int64_t tile = t0; tile < t1; ++tile) {
+        for (int r = 0; r < TILE_ROWS; ++r) {
+            const int64_t m = tile * TILE_ROWS + r;
+            const bool there = m < w.M;
+            for (int64_t g = 0; g < w.groups; ++g) {
+                const int64_t at = (tile * w.groups + g) * TILE_ROWS + r;
+                out_scales[at] = there ? scales[m * w.groups + g] : 0.0f;
+                if (out_zeros) out_zeros[at] = there ? zeros[m * w.groups + g] : 8;
+            }
+            for (int64_t b = 0; b < w.blocks; ++b) {
+                uint32_t *block = out_codes + (tile * w.blocks + b) * BLOCK_WORDS + r * 4;
+                for (int s = 0; s < 4; ++s) {
+                    for (int q = 0; q < 4; ++q) {
+                        const int64_t k = b * BLOCK_COLS + 32 * s + 8 * q;
+                        uint32_t v = 0;
+                        if (there && k + 8 <= w.K) {
+                            std::memcpy(&v, codes + m * row_bytes + k / 2, 4);
+                        } else {
+                            const uint32_t zero = there && zeros && w.groups > 0 ? zeros[m * w.groups + std::min<int64_t>(w.groups - 1, k / w.group)] : 8u;
+                            for (int j = 0; j < 8; ++j) {
+                                const uint32_t c = there && k + j < w.K ? (codes[m * row_bytes + (k + j) / 2] >> (4 * (j & 1))) & 15u : zero;
+                                v |= c << (4 * j);
+                            }
+                        }
+                        block[q * TILE_ROWS * 4 + s] = ordered(v);
+                    }
+                }
+            }
+        }
+    }
+}
+
+spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, const uint8_t *codes, const float *scales, const uint8_t *zeros)
+{
+    if (M < 0 || K < 0 || group < 1) return SPMM_ERR_INVALID_ARG;
+    if (M > MOST_ROWS || K > MOST_COLS || (group != 32 && group != 64 && group % BLOCK_COLS != 0)) return SPMM_ERR_UNSUPPORTED;
+    std::unique_ptr<spmm_quant> p(new spmm_quant);
+    quant_matrix &w = p->w;
+    w.M = M, w.K = K, w.group = group;
+    w.tiles = (int32_t)parts_of(M, TILE_ROWS), w.blocks = (int32_t)parts_of(K, BLOCK_COLS), w.groups = (int32_t)parts_of(K, group);
+    const int64_t n_scales = M * w.groups;
+    if (M > 0 && K > 0) {
+        if (!codes || !scales) return SPMM_ERR_INVALID_ARG;
+        for (int64_t i = 0; i < n_scales; ++i)
+            if (!std::isfinite(scales[i]) || (zeros && zeros[i] > 15)) return SPMM_ERR_INVALID_ARG;
+    }
+    hipError_t e = hipGetDevice(&p->device);
+    if (e != hipSuccess) return status_of(e);
+    const int64_t code_bytes = (int64_t)w.tiles * w.blocks * BLOCK_WORDS * 4, padded = (int64_t)w.tiles * w.groups * TILE_ROWS;
+    const int64_t scales_at = up_to(code_bytes, 256), zeros_at = scales_at + up_to(padded * 4, 256);
+    p->bytes = zeros_at + (zeros ? up_to(padded, 256) : 0);
+    if (code_bytes > 0) {
+        std::unique_ptr<char[]> host(new char[(size_t)p->bytes]);
+        uint32_t *out_codes = reinterpret_cast<uint32_t *>(host.get());
+        float *out_scales = reinterpret_cast<float *>(host.get() + scales_at);
+        uint8_t *out_zeros = zeros ? reinterpret_cast<uint8_t *>(host.get() + zeros_at) : nullptr;
+        // a thread for each MiB of codes, at most 16 and at most the machine's
+        const int64_t most = std::max<int64_t>(1, std::min<int64_t>(16, std::thread::hardware_concurrency()));
+        const int64_t threads = std::min<int64_t>(std::min(most, (int64_t)w.tiles), std::max<int64_t>(1, code_bytes >> 20));
+        std::vector<std::thread> others;
+        others.reserve((size_t)threads);
+        int64_t done = 0;
+        for (int64_t t = 0; t < threads; ++t) {
+            const int64_t t0 = w.tiles * t / threads, t1 = w.tiles * (t + 1) / threads;
+            auto work = [=, &w] { lay_out(w, t0, t1, codes, scales, zeros, out_codes, out_scales, out_zeros); };
+            if (t + 1 == threads) {
+                work();
+            } else {
+                try {
+                    others.emplace_back(work);
+                } catch (...) {  // no thread to be had: this one does it
+                    work();
+                }
+            }
+            done = t1;
+        }
+        for (std::thread &t : others) t.join();
+        if (done != w.tiles) return SPMM_ERR_ALLOC;
+        e = hipMalloc(reinterpret_cast<void **>(&p->memory), (size_t)p->bytes);
+        if (e != hipSuccess) {
+            (void)hipGetLastError();
+            p->memory = nullptr;
+            return SPMM_ERR_ALLOC;
+        }
+        e = hipMemcpy(p->memory, host.get(), (size_t)p->bytes, hipMemcpyHostToDevice);
+        if (e != hipSuccess) return status_of(e);
+        w.codes = reinterpret_cast<const uint32_t *>(p->memory);
+        w.scales = reinterpret_cast<const float *>(p->memory + scales_at);
+        w.zeros = zeros ? reinterpret_cast<const uint8_t *>(p->memory + zeros_at) : nullptr;
+    } else {
+        p->bytes = 0;
+    }
+    *plan = p.release();
+    return SPMM_OK;
+}
+
+template <typename F> spmm_status_t guarded(F &&f)
+{
+    try {
+        return f();
+    } catch (const std::bad_alloc &) {
+        return SPMM_ERR_ALLOC;
+    } catch (...) {
+        return SPMM_ERR_ALLOC;
+    }
+}
+
+bool extents(int64_t features, int64_t tokens) { return features >= 1 && features <= MOST_EXTENT && tokens >= 1 && tokens <= MOST_EXTENT; }
+
+bool room(const void *workspace, size_t bytes, int64_t needed)
+{
+    return needed == 0 || (workspace && (uintptr_t)workspace % 16 == 0 && bytes >= (size_t)needed);
+}
+
+// What norm and gate have in common: input, its optional companion, output and scales.
+spmm_status_t seen_rows(int64_t features, int64_t tokens, const spmm_tensor_t &x, const spmm_tensor_t &y, const spmm_tensor_t &out, float *scales, rows_args *a)
+{
+    if (!extents(features, tokens)) return SPMM_ERR_INVALID_ARG;
+    a->features = features, a->tokens = tokens;
+    spmm_status_t st = seen(x, features, tokens, &a->x);
+    if (st != SPMM_OK) return st;
+    if (x.type == SPMM_I8) return SPMM_ERR_INVALID_ARG;
+    if ((st = seen(out, features, tokens, &a->out)) != SPMM_OK) return st;
+    if (y.data) {
+        if (y.type != x.type) return SPMM_ERR_INVALID_ARG;
+        if ((st = seen(y, features, tokens, &a->y)) != SPMM_OK) return st;
+        if (!one_order(&a->y, a->x, features, tokens) && !one_order(&a->x, a->y, features, tokens)) return SPMM_ERR_UNSUPPORTED;
+    }
+    if (out.type == SPMM_I8) {
+        if (!scales || (uintptr_t)scales % 4 != 0) return SPMM_ERR_INVALID_ARG;
+        a->scales = scales;
+        if (!a->out.by_token) {
+            if (features != 1 || a->out.ld != tokens) return SPMM_ERR_UNSUPPORTED;
+            a->out = {a->out.data, 1, SPMM_I8, true};
+        }
+    } else if (!one_order(&a->out, a->x, features, tokens)) {
+        if (!one_order(&a->x, a->out, features, tokens) || (y.data && !one_order(&a->y, a->out, features, tokens))) return SPMM_ERR_UNSUPPORTED;
+    }
+    return SPMM_OK;
+}
+
+spmm_status_t seen_norm(int64_t K, int64_t N, const spmm_norm_t *args, rows_args *a)
+{
+    if (!args) return SPMM_ERR_INVALID_ARG;
+    *a = {};
+    spmm_status_t st = seen_rows(K, N, args->x, args->residual, args->out, args->scales, a);
+    if (st != SPMM_OK) return st;
+    if (!args->weight || args->weight_type < SPMM_F32 || args->weight_type > SPMM_BF16 || (uintptr_t)args->weight % (uintptr_t)size_of(args->weight_type) != 0 ||
+        !(args->eps >= 0.0f))
+        return SPMM_ERR_INVALID_ARG;
+    a->weight = static_cast<const char *>(args->weight), a->weight_type = args->weight_type, a->eps = args->eps;
+    if (args->total.data) {
+        if (args->total.type != args->x.type) return SPMM_ERR_INVALID_ARG;
+        if ((st = seen(args->total, K, N, &a->total)) != SPMM_OK) return st;
+        if (!one_order(&a->total, a->x, K, N)) return SPMM_ERR_UNSUPPORTED;
+    }
+    const span total = span_of(a->total, K, N), out = span_of(a->out, K, N), x = span_of(a->x, K, N), y = span_of(a->y, K, N);
+    const span weight = {a->weight, a->weight + K * size_of(a->weight_type)}, scales = {reinterpret_cast<char *>(a->scales), reinterpret_cast<char *>(a->scales + N)};
+    if (meet(out, x) || meet(out, y) || meet(out, total) || meet(out, weight) || meet(out, scales) || meet(total, weight) || meet(total, scales) || meet(scales, x) ||
+        meet(scales, y) || meet(scales, weight) || (meet(total, x) && !same(a->total, a->x)) || (meet(total, y) && !same(a->total, a->y)))
+        return SPMM_ERR_INVALID_ARG;
+    return SPMM_OK;
+}
+
+spmm_status_t seen_gate(int64_t F, int64_t N, const spmm_gate_t *args, rows_args *a)
+{
+    if (!args) return SPMM_ERR_INVALID_ARG;
+    *a = {};
+    const spmm_status_t st = seen_rows(F, N, args->a, args->b, args->out, args->scales, a);
+    if (st != SPMM_OK) return st;
+    if (args->act < SPMM_ACT_SILU || args->act > SPMM_ACT_RELU) return SPMM_ERR_INVALID_ARG;
+    a->act = args->act;
+    const span out = span_of(a->out, F, N), x = span_of(a->x, F, N), y = span_of(a->y, F, N);
+    const span scales = {reinterpret_cast<char *>(a->scales), reinterpret_cast<char *>(a->scales + N)};
+    if (meet(out, x) || meet(out, y) || meet(out, scales) || meet(scales, x) || meet(scales, y)) return SPMM_ERR_INVALID_ARG;
+    return SPMM_OK;
+}
+
+spmm_status_t run_rows(const rows_args &a, bool norm, void *workspace, size_t bytes, void *stream)
+{
+    if (!room(workspace, bytes, rows_workspace(a, norm))) return SPMM_ERR_INVALID_ARG;
+    return status_of(rows_launch(a, norm, static_cast<char *>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+spmm_status_t spmm_quant_create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, const uint8_t *codes, const float *scales, const uint8_t *zeros)
+{
+    if (!plan) return SPMM_ERR_INVALID_ARG;
+    *plan = nullptr;
+    return guarded([&] { return create(plan, M, K, group, codes, scales, zeros); });
+}
+
+spmm_status_t spmm_quant_destroy(spmm_quant_t *plan)
+{
+    delete plan;
+    return SPMM_OK;
+}
+
+spmm_status_t spmm_quant_describe(const spmm_quant_t *plan, int64_t *M, int64_t *K, int64_t *group, int64_t *device_bytes)
+{
+    if (!plan) return SPMM_ERR_INVALID_ARG;
+    if (M) *M = plan->w.M;
+    if (K) *K = plan->w.K;
+    if (group) *group = plan->w.group;
+    if (device_bytes) *device_bytes = plan->bytes;
+    return SPMM_OK;
+}
+
+spmm_status_t spmm_quant_workspace(const spmm_quant_t *plan, int32_t B_type, int64_t N, size_t *bytes)
+{
+    if (!plan || !bytes || B_type < SPMM_F32 || B_type > SPMM_I8 || N < 1 || N > MOST_EXTENT) return SPMM_ERR_INVALID_ARG;
+    *bytes = (size_t)quant_workspace(plan->w, B_type, N);
+    return SPMM_OK;
+}
+
+spmm_status_t spmm_quant_execute(const spmm_quant_t *plan, const spmm_tensor_t *B, const float *B_scales, int64_t N, const spmm_tensor_t *C, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    if (!plan || !B || !C || N < 1 || N > MOST_EXTENT) return SPMM_ERR_INVALID_ARG;
+    const quant_matrix &w = plan->w;
+    int device = -1;
+    if (hipGetDevice(&device) != hipSuccess || device != plan->device) {
+        (void)hipGetLastError();
+        return SPMM_ERR_INVALID_ARG;
+    }
+    if (B->type < SPMM_F32 || B->type > SPMM_I8 || C->type < SPMM_F32 || C->type > SPMM_BF16) return SPMM_ERR_INVALID_ARG;
+    if (w.M == 0) return SPMM_OK;
+    tensor b = {}, c = {};
+    spmm_status_t st = SPMM_OK;
+    if (w.K > 0 && (st = seen(*B, w.K, N, &b)) != SPMM_OK) return st;
+    if (w.K == 0) b.type = B->type;
+    if ((st = seen(*C, w.M, N, &c)) != SPMM_OK) return st;
+    if (b.type == SPMM_I8) {
+        if (!B_scales || (uintptr_t)B_scales % 4 != 0) return SPMM_ERR_INVALID_ARG;
+        if (w.K > 0 && !b.by_token) {
+            if (w.K != 1 || b.ld != N) return SPMM_ERR_UNSUPPORTED;
+            b = {b.data, 1, SPMM_I8, true};
+        }
+    }
+    if (meet(span_of(b, w.K, N), span_of(c, w.M, N))) return SPMM_ERR_INVALID_ARG;
+    if (!room(workspace, workspace_bytes, quant_workspace(w, b.type, N))) return SPMM_ERR_INVALID_ARG;
+    return status_of(quant_execute(w, b, b.type == SPMM_I8 ? B_scales : nullptr, N, c, static_cast<char *>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+spmm_status_t spmm_norm_workspace(int64_t K, int64_t N, const spmm_norm_t *args, size_t *bytes)
+{
+    rows_args a;
+    if (!bytes) return SPMM_ERR_INVALID_ARG;
+    const spmm_status_t st = seen_norm(K, N, args, &a);
+    if (st == SPMM_OK) *bytes = (size_t)rows_workspace(a, true);
+    return st;
+}
+
+spmm_status_t spmm_norm(int64_t K, int64_t N, const spmm_norm_t *args, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rows_args a;
+    const spmm_status_t st = seen_norm(K, N, args, &a);
+    return st == SPMM_OK ? run_rows(a, true, workspace, workspace_bytes, stream) : st;
+}
+
+spmm_status_t spmm_gate_workspace(int64_t F, int64_t N, const spmm_gate_t *args, size_t *bytes)
+{
+    rows_args a;
+    if (!bytes) return SPMM_ERR_INVALID_ARG;
+    const spmm_status_t st = seen_gate(F, N, args, &a);
+    if (st == SPMM_OK) *bytes = (size_t)rows_workspace(a, false);
+    return st;
+}
+
+spmm_status_t spmm_gate(int64_t F, int64_t N, const spmm_gate_t *args, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rows_args a;
+    const spmm_status_t st = seen_gate(F, N, args, &a);
+    return st == SPMM_OK ? run_rows(a, false, workspace, workspace_bytes, stream) : st;
+}
+
+}  // extern "C"
