@@ -1,9 +1,16 @@
 // What stands between two products (gfx950): the root-mean-square norm with the residual's addition, and the gated
 // activation, both with floating output or in 8-bit codes with a scale a token.
 //
-// A workgroup has all features of its tokens: a first pass makes the sum of squares and the largest magnitude (of
-// values without the token's common factor, so that codes do not wait for it), a second one the output.
+//   norm  t = x + r, rounded;  p = t w;    f = 1 / sqrt(mean t^2 + eps)
+//   gate                       p = act(a) b;  f = 1
+//   out = p f (norm: t f w), or code = rint(p (127 / max |p|)), scale = max |p| f / 127
+//
+// Codes do not wait for f: they depend on p alone, so one look at the token gives both statistics.  All of it is bound by
+// memory, or by the latency of one launch: elements are read once and held in registers between the statistics
+// and the output (rows_kernel, columns_kernel), up to the lengths that their registers hold.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "../../../include/spmm_layers.h"
 #include "../spmm_launch.h"
@@ -13,76 +20,302 @@
 namespace layers {
 namespace {
 
-constexpr int THREADS = 256;
-
+// x / (1 + exp(-u)): silu for u = x; gelu for u = 2 sqrt(2 / pi) (x + 0.044715 x^3), since (1 + tanh(u / 2)) / 2 = 1 / (1 + exp(-u)), which does not
+// cancel for negative x.  The exponential by its base-2 instruction (its argument's rounding is worth |u| 2^-24 of the result), the quotient
+// by the reciprocal's: both are right to a unit of the last place.
 __device__ inline float act_of(float x, int32_t act)
 {
-    if (act == SPMM_ACT_SILU) return x / (1.0f + expf(-x));
-    if (act == SPMM_ACT_GELU) return x / (1.0f + expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));  // 1 + tanh(u) = 2 / (1 + exp(-2 u)), which does not cancel
-    return x < 0.0f ? 0.0f : x;
+    if (act == SPMM_ACT_RELU) return x < 0.0f ? 0.0f : x;
+    const float u = act == SPMM_ACT_SILU ? x : 1.5957691216057308f * (x + 0.044715f * x * x * x);
+    return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u));
 }
 
-// The larger magnitude; an infinity or a NaN stays one.
+// The larger magnitude; an infinity or a NaN counts as an infinity.
 __device__ inline float larger(float most, float v)
 {
     const float m = fabsf(v);
     return m <= most ? most : m != m ? __builtin_inff() : m;
 }
 
-template <bool NORM, int TYPE> __device__ inline float value_of(const rows_args &a, int64_t at, int64_t k)
+// What a token's codes and values are made with.
+struct token_factors {
+    float factor;     // f
+    float up, steps;  // code = rint(p * up * steps); up keeps 127 / max |p| finite for the smallest values
+    float scale;
+    __device__ token_factors(bool norm, float square, float most, const rows_args &a)
+    {
+        factor = norm ? 1.0f / sqrtf(square / (float)a.features + a.eps) : 1.0f;
+        up = most < 0x1p-100f ? 0x1p100f : 1.0f;
+        steps = most > 0.0f && most < __builtin_inff() ? 127.0f / (most * up) : 0.0f;
+        scale = most < __builtin_inff() ? most * factor / 127.0f : __builtin_nanf("");
+    }
+    __device__ int8_t code(float p) const { return steps == 0.0f ? (int8_t)0 : (int8_t)rintf(p * up * steps); }
+};
+
+// Elements from `at` on of x and, where there is one, of its companion: t (norm, rounded to x's type) or p (gate).
+template <bool NORM, int TYPE, int N> __device__ inline void values_at(const rows_args &a, int64_t x_at, int64_t y_at, int there, float (&v)[N])
 {
-    const float x = load_as(a.x.data, at, TYPE);
-    if constexpr (NORM) {
-        if (!a.y.data) return x;
-        typename element<TYPE>::type t = (typename element<TYPE>::type)(x + load_as(a.y.data, at, TYPE));
-        return (float)t;
-    } else {
-        return act_of(x, a.act) * (a.y.data ? load_as(a.y.data, at, TYPE) : 1.0f);
+    typedef typename element<TYPE>::type T;
+    float y[N];
+    load_row<T>(a.x.data, x_at, there, v);
+    if (a.y.data) load_row<T>(a.y.data, y_at, there, y);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if constexpr (NORM) {
+            if (a.y.data) v[j] = (float)(T)(v[j] + y[j]);
+        } else {
+            v[j] = act_of(v[j], a.act) * (a.y.data ? y[j] : 1.0f);
+        }
     }
 }
 
-// TOKENS tokens a workgroup, THREADS / TOKENS threads each.
-template <bool NORM, int TYPE, int TOKENS> __global__ __launch_bounds__(THREADS) void rows_kernel(rows_args a)
+template <bool SQUARE, bool MOST> __device__ inline void reduce_lanes(float &square, float &most, int from)
 {
-    constexpr int EACH = THREADS / TOKENS;
-    __shared__ float squares[EACH][TOKENS], mosts[EACH][TOKENS];
-    const int token = threadIdx.x % TOKENS, part = threadIdx.x / TOKENS;
-    const int64_t n = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * TOKENS + token;
-    const bool there = n < a.tokens;
-    auto at = [&](const tensor &t, int64_t k) { return t.by_token ? n * t.ld + k : k * t.ld + n; };
+    for (int d = from; d < 64; d *= 2) {
+        if constexpr (SQUARE) square += __shfl_xor(square, d);
+        if constexpr (MOST) most = fmaxf(most, __shfl_xor(most, d));
+    }
+}
+
+// ---- a token a row of memory -----------------------------------------------------------------------------------
+
+constexpr int UNIT = 8;  // neighbouring elements of a thread: 16 bytes of 16-bit elements
+
+// T threads a token, TOKENS tokens a workgroup; every thread holds R units.
+template <bool NORM, bool CODES, int TYPE, int T, int R, int TOKENS> __global__ __launch_bounds__(T *TOKENS) void rows_kernel(rows_args a)
+{
+    typedef typename element<TYPE>::type E;
+    constexpr int WAVES = T / 64;
+    constexpr bool KEEP_WEIGHTS = NORM && !CODES && R <= 2;  // (with codes p is kept in t's place; longer ones read the weights again)
+    __shared__ float squares[WAVES * TOKENS], mosts[WAVES * TOKENS];
+    const int t = threadIdx.x % T;
+    const int64_t n = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * TOKENS + threadIdx.x / T;
+    if (n >= a.tokens) return;  // (a workgroup of several waves has one token)
+    auto unit = [&](int i) { return ((int64_t)i * T + t) * UNIT; };
+    auto there = [&](int i) { return (int)min((int64_t)UNIT, max((int64_t)0, a.features - unit(i))); };
+    float v[R][UNIT], w[R][UNIT];
+#pragma unroll
+    for (int i = 0; i < R; ++i) values_at<NORM, TYPE>(a, n * a.x.ld + unit(i), n * a.y.ld + unit(i), there(i), v[i]);
+    if constexpr (NORM && (CODES || KEEP_WEIGHTS)) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) load_row_as(a.weight, unit(i), there(i), a.weight_type, w[i]);
+    }
     float square = 0.0f, most = 0.0f;
-    if (there) {
-        for (int64_t k = part; k < a.features; k += EACH) {
-            float v = value_of<NORM, TYPE>(a, at(a.x, k), k);
-            if constexpr (NORM) {
-                if (a.total.data) store_as(a.total.data, at(a.total, k), TYPE, v);
-                square += v * v;
-                v *= load_as(a.weight, k, a.weight_type);
-            }
-            most = larger(most, v);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if constexpr (NORM)
+            if (a.total.data) store_row<E>(a.total.data, n * a.total.ld + unit(i), there(i), v[i]);
+#pragma unroll
+        for (int j = 0; j < UNIT; ++j) {
+            if constexpr (NORM) square += v[i][j] * v[i][j];
+            if constexpr (NORM && CODES) v[i][j] *= w[i][j];
+            if constexpr (CODES) most = larger(most, v[i][j]);
         }
     }
-    squares[part][token] = square;
-    mosts[part][token] = most;
+    reduce_lanes<NORM, CODES>(square, most, 1);
+    if constexpr (WAVES > 1) {
+        if ((t & 63) == 0) squares[t / 64] = square, mosts[t / 64] = most;
+        __syncthreads();
+        square = squares[0], most = mosts[0];
+#pragma unroll
+        for (int wave = 1; wave < WAVES; ++wave) square += squares[wave], most = fmaxf(most, mosts[wave]);
+    }
+    const token_factors f(NORM, square, most, a);
+    if (CODES && t == 0) a.scales[n] = f.scale;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if constexpr (CODES) {
+#pragma unroll
+            for (int j = 0; j < UNIT; ++j) v[i][j] = (float)f.code(v[i][j]);
+            store_row<int8_t>(a.out.data, n * a.out.ld + unit(i), there(i), v[i]);
+        } else {
+            if constexpr (!KEEP_WEIGHTS) load_row_as(a.weight, unit(i), there(i), a.weight_type, w[i]);
+#pragma unroll
+            for (int j = 0; j < UNIT; ++j) v[i][j] = v[i][j] * f.factor * w[i][j];
+            store_row_as(a.out.data, n * a.out.ld + unit(i), there(i), a.out.type, v[i]);
+        }
+    }
+}
+
+// Tokens longer than a workgroup holds: read twice (the second time the sum, where it was written: it may be x's own memory).
+template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(1024) void long_rows_kernel(rows_args a)
+{
+    typedef typename element<TYPE>::type E;
+    __shared__ float squares[16], mosts[16];
+    const int t = threadIdx.x;
+    const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (n >= a.tokens) return;
+    float square = 0.0f, most = 0.0f;
+    for (int64_t k = t * UNIT; k < a.features; k += 1024 * UNIT) {
+        const int there = (int)min((int64_t)UNIT, a.features - k);
+        float v[UNIT], w[UNIT];
+        values_at<NORM, TYPE>(a, n * a.x.ld + k, n * a.y.ld + k, there, v);
+        if constexpr (NORM)
+            if (a.total.data) store_row<E>(a.total.data, n * a.total.ld + k, there, v);
+        if constexpr (NORM && CODES) load_row_as(a.weight, k, there, a.weight_type, w);
+#pragma unroll
+        for (int j = 0; j < UNIT; ++j) {
+            if constexpr (NORM) square += v[j] * v[j];
+            if constexpr (CODES) most = larger(most, NORM ? v[j] * w[j] : v[j]);
+        }
+    }
+    reduce_lanes<NORM, CODES>(square, most, 1);
+    if ((t & 63) == 0) squares[t / 64] = square, mosts[t / 64] = most;
     __syncthreads();
-    square = most = 0.0f;
-    for (int p = 0; p < EACH; ++p) {
-        square += squares[p][token];
-        most = larger(most, mosts[p][token]);
+    square = squares[0], most = mosts[0];
+    for (int wave = 1; wave < 16; ++wave) square += squares[wave], most = fmaxf(most, mosts[wave]);
+    const token_factors f(NORM, square, most, a);
+    if (CODES && t == 0) a.scales[n] = f.scale;
+    for (int64_t k = t * UNIT; k < a.features; k += 1024 * UNIT) {
+        const int there = (int)min((int64_t)UNIT, a.features - k);
+        float v[UNIT], w[UNIT];
+        if (NORM && a.total.data) load_row<E>(a.total.data, n * a.total.ld + k, there, v);
+        else values_at<NORM, TYPE>(a, n * a.x.ld + k, n * a.y.ld + k, there, v);
+        if constexpr (NORM) load_row_as(a.weight, k, there, a.weight_type, w);
+#pragma unroll
+        for (int j = 0; j < UNIT; ++j) v[j] = CODES ? (float)f.code(NORM ? v[j] * w[j] : v[j]) : v[j] * f.factor * w[j];
+        if constexpr (CODES) store_row<int8_t>(a.out.data, n * a.out.ld + k, there, v);
+        else store_row_as(a.out.data, n * a.out.ld + k, there, a.out.type, v);
     }
-    if (!there) return;
-    const float factor = NORM ? 1.0f / sqrtf(square / (float)a.features + a.eps) : 1.0f;
-    const bool codes = a.out.type == SPMM_I8;
-    // 127 / most overflows for the smallest values: those are made larger first
-    const float up = most < 0x1p-100f ? 0x1p100f : 1.0f;
-    const float steps = most > 0.0f && most < __builtin_inff() ? 127.0f / (most * up) : 0.0f;
-    if (codes && part == 0) a.scales[n] = most < __builtin_inff() ? most * factor / 127.0f : __builtin_nanf("");
-    for (int64_t k = part; k < a.features; k += EACH) {
-        float v = NORM && a.total.data ? load_as(a.total.data, at(a.total, k), TYPE) : value_of<NORM, TYPE>(a, at(a.x, k), k);
-        const float w = NORM ? load_as(a.weight, k, a.weight_type) : 1.0f;
-        if (codes) reinterpret_cast<int8_t *>(a.out.data)[at(a.out, k)] = steps == 0.0f ? 0 : (int8_t)rintf(v * w * up * steps);
-        else store_as(a.out.data, at(a.out, k), a.out.type, v * factor * w);
+}
+
+// ---- a feature a row of memory ---------------------------------------------------------------------------------
+
+// A workgroup has all features of 16 tokens.  A thread reads 16 bytes of a row, COLS threads lie side by side (64 or 32 bytes of a row), ROWS rows are read
+// at a time; HELD such steps stay in registers (0: any number of them, read twice).
+template <int TYPE> constexpr int COLUMN_UNIT = TYPE == SPMM_F32 ? 4 : 8;
+constexpr int COLUMN_TOKENS = 16, COLUMN_THREADS = 1024;
+template <int TYPE> constexpr int COLUMN_ROWS = COLUMN_THREADS / (COLUMN_TOKENS / COLUMN_UNIT<TYPE>);
+
+template <bool NORM, bool CODES, int TYPE, int HELD> __global__ __launch_bounds__(COLUMN_THREADS) void columns_kernel(rows_args a)
+{
+    typedef typename element<TYPE>::type E;
+    constexpr int U = COLUMN_UNIT<TYPE>, COLS = COLUMN_TOKENS / U, ROWS = COLUMN_ROWS<TYPE>, WAVES = COLUMN_THREADS / 64;
+    __shared__ float squares[WAVES][COLUMN_TOKENS], mosts[WAVES][COLUMN_TOKENS], factors[2][COLUMN_TOKENS];
+    __shared__ int8_t turned[CODES ? 2 : 1][CODES ? COLUMN_TOKENS : 1][ROWS + 4];
+    const int col = threadIdx.x % COLS, row = threadIdx.x / COLS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t n0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * COLUMN_TOKENS, n = n0 + col * U;
+    if (n0 >= a.tokens) return;
+    const int wide = (int)min((int64_t)U, max((int64_t)0, a.tokens - n));
+    float square[U], most[U], held[HELD ? HELD : 1][U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) square[j] = most[j] = 0.0f;
+    auto weight_of = [&](int64_t k) {
+        float w[1] = {0.0f};
+        if (NORM && k < a.features) load_row_as(a.weight, k, 1, a.weight_type, w);
+        return w[0];
+    };
+    auto look = [&](int64_t k, float (&v)[U]) {
+        if constexpr (NORM)
+            if (a.total.data && k < a.features) store_row<E>(a.total.data, k * a.total.ld + n, wide, v);
+        const float w = NORM && CODES ? weight_of(k) : 1.0f;
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if constexpr (NORM) square[j] += v[j] * v[j];
+            if constexpr (NORM && CODES) v[j] *= w;  // p in t's place
+            if constexpr (CODES) most[j] = larger(most[j], v[j]);
+        }
+    };
+    if constexpr (HELD > 0) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const int64_t k = (int64_t)i * ROWS + row;
+            values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, k < a.features ? wide : 0, held[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) look((int64_t)i * ROWS + row, held[i]);
+    } else {
+        for (int64_t k = row; k < a.features; k += ROWS) {
+            values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, wide, held[0]);
+            look(k, held[0]);
+        }
     }
+#pragma unroll
+    for (int j = 0; j < U; ++j) reduce_lanes<NORM, CODES>(square[j], most[j], COLS);
+    if (lane < COLS) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) squares[wave][lane * U + j] = square[j], mosts[wave][lane * U + j] = most[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < COLUMN_TOKENS && n0 + threadIdx.x < a.tokens) {  // a thread a token
+        float s = squares[0][threadIdx.x], m = mosts[0][threadIdx.x];
+        for (int w = 1; w < WAVES; ++w) s += squares[w][threadIdx.x], m = fmaxf(m, mosts[w][threadIdx.x]);
+        const token_factors f(NORM, s, m, a);
+        if (CODES) a.scales[n0 + threadIdx.x] = f.scale;
+        factors[0][threadIdx.x] = CODES ? f.up : f.factor;
+        factors[1][threadIdx.x] = f.steps;
+    }
+    __syncthreads();
+    float first[U], second[U];  // f, or the two factors of codes
+#pragma unroll
+    for (int j = 0; j < U; ++j) first[j] = factors[0][col * U + j], second[j] = factors[1][col * U + j];
+    // (with codes v is p)
+    auto write = [&](int64_t k0, int step, const float (&v)[U]) {
+        const int64_t k = k0 + row;
+        if constexpr (!CODES) {
+            const float w = weight_of(k);
+            float c[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) c[j] = v[j] * first[j] * w;
+            if (k < a.features) store_row_as(a.out.data, k * a.out.ld + n, wide, a.out.type, c);
+        } else {
+            // codes change places through LDS: a row of memory is a token there.  Two places in turn, so that one barrier a step is enough.
+            int8_t(&tile)[COLUMN_TOKENS][ROWS + 4] = turned[step & 1];
+#pragma unroll
+            for (int j = 0; j < U; ++j) tile[col * U + j][row] = second[j] == 0.0f ? (int8_t)0 : (int8_t)rintf(v[j] * first[j] * second[j]);
+            __syncthreads();
+            constexpr int EACH = COLUMN_TOKENS * ROWS / COLUMN_THREADS;  // 4 or 8 codes of a token
+            const int token = threadIdx.x / (ROWS / EACH), r = threadIdx.x % (ROWS / EACH) * EACH;
+            const int there = (int)min((int64_t)EACH, max((int64_t)0, a.features - k0 - r));
+            if (n0 + token < a.tokens) {
+                int8_t *to = reinterpret_cast<int8_t *>(a.out.data) + (n0 + token) * a.out.ld + k0 + r;
+                if (there == EACH) {
+                    *reinterpret_cast<neighbours<int8_t, EACH> *>(to) = *reinterpret_cast<const neighbours<int8_t, EACH> *>(&tile[token][r]);
+                } else {
+                    for (int j = 0; j < there; ++j) to[j] = tile[token][r + j];
+                }
+            }
+        }
+    };
+    if constexpr (HELD > 0) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) write((int64_t)i * ROWS, i, held[i]);
+    } else {
+        int step = 0;
+        for (int64_t k0 = 0; k0 < a.features; k0 += ROWS, ++step) {
+            const int64_t k = k0 + row;
+            const int there = k < a.features ? wide : 0;
+            if (NORM && a.total.data) load_row<E>(a.total.data, k * a.total.ld + n, there, held[0]);
+            else values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, there, held[0]);
+            if constexpr (NORM && CODES) {
+                const float w = weight_of(k);
+#pragma unroll
+                for (int j = 0; j < U; ++j) held[0][j] *= w;
+            }
+            write(k0, step, held[0]);
+        }
+    }
+}
+
+// ---- the gate with floating output: element by element ---------------------------------------------------------
+
+// `rows` rows of memory of `units` units each; short rows without gaps have been made one long row by the launch.
+template <int TYPE> __global__ __launch_bounds__(256) void elements_kernel(rows_args a, int64_t rows, int64_t length, uint32_t units)
+{
+    const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+    int64_t row, unit;
+    if (rows == 1) {
+        row = 0, unit = at;
+    } else {
+        row = at >> 32 ? at / units : (int64_t)((uint32_t)at / units);
+        unit = at - row * units;
+    }
+    if (row >= rows || unit * UNIT >= length) return;
+    const int64_t k = unit * UNIT;
+    const int there = (int)min((int64_t)UNIT, length - k);
+    float v[UNIT];
+    values_at<false, TYPE>(a, row * a.x.ld + k, row * a.y.ld + k, there, v);
+    store_row_as(a.out.data, row * a.out.ld + k, there, a.out.type, v);
 }
 
 // A launch has less than 2^32 threads along an axis.
@@ -92,18 +325,42 @@ dim3 grid_of(int64_t blocks)
     return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
 }
 
-template <bool NORM> hipError_t launch(const rows_args &a, hipStream_t stream)
+template <int TYPE> hipError_t launch_elements(const rows_args &a, hipStream_t stream)
 {
-    auto run = [&](auto type) {
-        constexpr int TYPE = decltype(type)::value;
-        if (a.x.by_token) return launch_kernel(rows_kernel<NORM, TYPE, 1>, grid_of(a.tokens), THREADS, 0, stream, a);
-        return launch_kernel(rows_kernel<NORM, TYPE, 16>, grid_of((a.tokens + 15) / 16), THREADS, 0, stream, a);
-    };
-    switch (a.x.type) {
-    case SPMM_F32: return run(std::integral_constant<int, SPMM_F32>());
-    case SPMM_F16: return run(std::integral_constant<int, SPMM_F16>());
-    default: return run(std::integral_constant<int, SPMM_BF16>());
+    int64_t rows = a.x.by_token ? a.tokens : a.features, length = a.x.by_token ? a.features : a.tokens;
+    if (rows == 1 || (a.x.ld == length && a.out.ld == length && (!a.y.data || a.y.ld == length))) length *= rows, rows = 1;
+    const int64_t units = (length + UNIT - 1) / UNIT;
+    return launch_kernel(elements_kernel<TYPE>, grid_of((rows * units + 255) / 256), 256, 0, stream, a, rows, length, (uint32_t)units);
+}
+
+template <bool NORM, bool CODES, int TYPE> hipError_t launch(const rows_args &a, hipStream_t stream)
+{
+    const int64_t K = a.features, N = a.tokens;
+    if (!a.x.by_token) {
+        const dim3 grid = grid_of((N + COLUMN_TOKENS - 1) / COLUMN_TOKENS);
+        if (K <= COLUMN_ROWS<TYPE>) return launch_kernel(columns_kernel<NORM, CODES, TYPE, 1>, grid, COLUMN_THREADS, 0, stream, a);
+        if (K <= 4 * COLUMN_ROWS<TYPE>) return launch_kernel(columns_kernel<NORM, CODES, TYPE, 4>, grid, COLUMN_THREADS, 0, stream, a);
+        return launch_kernel(columns_kernel<NORM, CODES, TYPE, 0>, grid, COLUMN_THREADS, 0, stream, a);
     }
+    const int64_t units = (K + UNIT - 1) / UNIT;
+    if (units <= 64) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 64, 1, 4>, grid_of((N + 3) / 4), 256, 0, stream, a);
+    if (units <= 256) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 256, 1, 1>, grid_of(N), 256, 0, stream, a);
+    // Few tokens are over when their slowest is: more threads each.  Many are a matter of bandwidth, which smaller workgroups, of which a compute unit has
+    // several in different phases, come nearer to.
+    const bool few = N <= 512;
+    if (units <= 512 && !few) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 256, 2, 1>, grid_of(N), 256, 0, stream, a);
+    if (units <= 1024 && !few) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 256, 4, 1>, grid_of(N), 256, 0, stream, a);
+    if (units <= 1024) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 1024, 1, 1>, grid_of(N), 1024, 0, stream, a);
+    if (units <= 2048) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 1024, 2, 1>, grid_of(N), 1024, 0, stream, a);
+    if (units <= 4096) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 1024, 4, 1>, grid_of(N), 1024, 0, stream, a);
+    return launch_kernel(long_rows_kernel<NORM, CODES, TYPE>, grid_of(N), 1024, 0, stream, a);
+}
+
+template <int TYPE> hipError_t launch_type(const rows_args &a, bool norm, hipStream_t stream)
+{
+    const bool codes = a.out.type == SPMM_I8;
+    if (norm) return codes ? launch<true, true, TYPE>(a, stream) : launch<true, false, TYPE>(a, stream);
+    return codes ? launch<false, true, TYPE>(a, stream) : launch_elements<TYPE>(a, stream);
 }
 
 }  // namespace
@@ -112,7 +369,11 @@ int64_t rows_workspace(const rows_args &, bool) { return 0; }
 
 hipError_t rows_launch(const rows_args &a, bool norm, char *, hipStream_t stream)
 {
-    return norm ? launch<true>(a, stream) : launch<false>(a, stream);
+    switch (a.x.type) {
+    case SPMM_F32: return launch_type<SPMM_F32>(a, norm, stream);
+    case SPMM_F16: return launch_type<SPMM_F16>(a, norm, stream);
+    default: return launch_type<SPMM_BF16>(a, norm, stream);
+    }
 }
 
 }  // namespace layers
