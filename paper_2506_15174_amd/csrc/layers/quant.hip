@@ -10,6 +10,8 @@
 // pack_kernel lays B out as the instructions take it; product_kernel gives a tile of 16 rows and up to 128 tokens to a workgroup, whose waves share K.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "../../../include/spmm_layers.h"
 #include "../spmm_launch.h"
 #include "elements.h"
@@ -39,49 +41,89 @@ constexpr int WAVES = 8;
 // codes hold two steps in the 16 bytes of a lane: [token tile][block][pair of steps][lane][step][8 columns].
 // Lane 16 q + t holds token t, columns 32 s + 8 q + j.  Tokens and columns that do not exist are zeros.
 
+// Eight columns of a token as operands: a part each; codes are eight bytes.
+template <int BT> struct operands {
+    u32x4 part[PARTS<BT>];
+};
+template <> struct operands<SPMM_I8> {
+    u32x2 part[1];
+};
+
+// fp32: each part is the upper half of what is left, cut off, not rounded, so that large values stay finite.  An infinity or a NaN is the first
+// part's alone.
+__device__ inline void split(const float (&v)[8], operands<SPMM_F32> &o)
+{
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        uint32_t bits[2][3];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float x = v[j + h];
+            const bool finite = __builtin_isfinite(x);
+            const uint32_t b0 = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
+            const float left1 = x - __builtin_bit_cast(float, b0);
+            const uint32_t b1 = __builtin_bit_cast(uint32_t, left1) & 0xffff0000u;
+            const float left2 = left1 - __builtin_bit_cast(float, b1);
+            bits[h][0] = x != x ? 0x7fc00000u : b0;
+            bits[h][1] = finite ? b1 : 0;
+            bits[h][2] = finite ? __builtin_bit_cast(uint32_t, left2) : 0;
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) o.part[p][j / 2] = __builtin_amdgcn_perm(bits[1][p], bits[0][p], 0x07060302u);
+    }
+}
+
+// Columns k0 .. k0 + 7 of token n, of which `there` exist (the others are 0).
+template <int BT> __device__ inline void fetch(const tensor &B, int64_t n, int64_t k0, int there, operands<BT> &o)
+{
+    const int64_t stride = B.by_token ? 1 : B.ld, at = B.by_token ? n * B.ld + k0 : k0 * B.ld + n;
+    if constexpr (BT == SPMM_I8) {
+        u32x2 raw = {0, 0};  // (codes lie one token a row)
+        if (there >= 8) {
+            raw = __builtin_bit_cast(u32x2, *reinterpret_cast<const neighbours<int8_t, 8> *>(B.data + at));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < there) raw[j / 4] |= (uint32_t) reinterpret_cast<const uint8_t *>(B.data)[at + j] << (8 * (j % 4));
+        }
+        // the order in which the weights' nibbles become bytes: 0 4 1 5, 2 6 3 7
+        o.part[0] = u32x2{__builtin_amdgcn_perm(raw[1], raw[0], 0x05010400u), __builtin_amdgcn_perm(raw[1], raw[0], 0x07030602u)};
+    } else if constexpr (BT == SPMM_F32) {
+        float v[8];
+        if (B.by_token) {
+            load_row<float>(B.data, at, there, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < there ? reinterpret_cast<const float *>(B.data)[at + j * stride] : 0.0f;
+        }
+        split(v, o);
+    } else {
+        if (B.by_token && there >= 8) {
+            o.part[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const neighbours<uint16_t, 8> *>(B.data + 2 * at));
+        } else {
+            u32x4 word = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t v = j < there ? reinterpret_cast<const uint16_t *>(B.data)[at + j * stride] : 0;
+                word[j / 2] |= v << (16 * (j & 1));
+            }
+            o.part[0] = word;
+        }
+    }
+}
+
 template <int BT> __global__ __launch_bounds__(256) void pack_kernel(tensor B, int64_t K, int64_t N, int32_t blocks, char *out)
 {
     const int lane = threadIdx.x & 63, s = threadIdx.x >> 6, t = lane & 15, q = lane >> 4;
     const int64_t block = blockIdx.x, tile = blockIdx.y, n = tile * 16 + t, k0 = block * BLOCK_COLS + 32 * s + 8 * q;
-    const int64_t stride = B.by_token ? 1 : B.ld, at = B.by_token ? n * B.ld + k0 : k0 * B.ld + n;
-    const int there = n < N ? (int)min((int64_t)8, K - k0) : 0;
     char *block_out = out + (tile * blocks + block) * (4 * PARTS<BT> * STEP_BYTES<BT>);
+    operands<BT> o;
+    fetch<BT>(B, n, k0, n < N ? (int)min((int64_t)8, K - k0) : 0, o);
     if constexpr (BT == SPMM_I8) {
-        // the order in which the weights' nibbles become bytes
-        constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};
-        int8_t v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < there ? reinterpret_cast<const int8_t *>(B.data)[at + j * stride] : 0;
-        u32x2 word = {0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) word[j / 4] |= (uint32_t)(uint8_t)v[order[j]] << (8 * (j % 4));
-        *reinterpret_cast<u32x2 *>(block_out + (s >> 1) * 1024 + lane * 16 + (s & 1) * 8) = word;
-    } else if constexpr (BT == SPMM_F32) {
-        u32x4 parts[3];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            // Each part is the upper half of what is left: cut off, not rounded, so that large values stay finite.  An infinity or a NaN
-            // is the first part's alone.
-            const float v = j < there ? reinterpret_cast<const float *>(B.data)[at + j * stride] : 0.0f;
-            float left = v;
-#pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                uint32_t bits = __builtin_bit_cast(uint32_t, left) & 0xffff0000u;
-                if (p == 0 && v != v) bits = 0x7fc00000u;
-                parts[p][j / 2] = (j & 1) ? parts[p][j / 2] | bits : bits >> 16;
-                left = __builtin_isfinite(v) ? left - __builtin_bit_cast(float, bits) : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4 *>(block_out + (s * 3 + p) * 1024 + lane * 16) = parts[p];
+        *reinterpret_cast<u32x2 *>(block_out + (s >> 1) * 1024 + lane * 16 + (s & 1) * 8) = o.part[0];
     } else {
-        u32x4 word = {0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t v = j < there ? reinterpret_cast<const uint16_t *>(B.data)[at + j * stride] : 0;
-            word[j / 2] |= v << (16 * (j & 1));
-        }
-        *reinterpret_cast<u32x4 *>(block_out + s * 1024 + lane * 16) = word;
+        for (int p = 0; p < PARTS<BT>; ++p) *reinterpret_cast<u32x4 *>(block_out + (s * PARTS<BT> + p) * 1024 + lane * 16) = o.part[p];
     }
 }
 
@@ -231,8 +273,126 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
     }
 }
 
+// ---- few tokens ------------------------------------------------------------------------------------------------
+//
+// Up to 16 tokens are one tile, and a product is over in the time of a few memory accesses: one launch, in which every wave reads its columns of
+// B as it reads its weights and makes operands of them itself.  Lanes of tokens that do not exist read the last one's (an access the
+// wave makes anyway); their results are not stored.  Weights, scales and B of AHEAD blocks are asked for before the first is used.
+// PER_GROUP: steps of 32 columns behind which a group's sum is full (4, 2 or 1).
+
+template <int BT, int PER_GROUP, int KWAVES> __global__ __launch_bounds__(64 * KWAVES) void few_kernel(quant_matrix W, tensor B, const float *B_scales, int32_t N, tensor C)
+{
+    __shared__ float sums[KWAVES][256];
+    constexpr int AHEAD = BT == SPMM_F32 ? 1 : 2, SUMS = 4 / PER_GROUP;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4, n = min(r, N - 1);
+    const int64_t row_tile = blockIdx.x;
+    const int group_blocks = PER_GROUP < 4 ? 1 : (int)(W.group / BLOCK_COLS);
+    const uint32_t *codes = W.codes + row_tile * W.blocks * BLOCK_WORDS + lane * 4;
+    const float *scales = W.scales + row_tile * W.groups * TILE_ROWS + r;
+    const uint8_t *zeros = W.zeros ? W.zeros + row_tile * W.groups * TILE_ROWS + r : nullptr;
+    const int first = (int)((int64_t)W.blocks * wave / KWAVES), last = (int)((int64_t)W.blocks * (wave + 1) / KWAVES);
+    struct asked {
+        u32x4 word;
+        float scale[SUMS];
+        int zero[SUMS];
+        operands<BT> b[4];
+    };
+    auto ask = [&](int b, asked &a) {
+        a.word = *reinterpret_cast<const u32x4 *>(codes + (int64_t)b * BLOCK_WORDS);
+#pragma unroll
+        for (int g = 0; g < SUMS; ++g) {
+            const int group = PER_GROUP < 4 ? min(W.groups - 1, b * SUMS + g) : b / group_blocks;
+            a.scale[g] = scales[group * TILE_ROWS];
+            a.zero[g] = zeros ? zeros[group * TILE_ROWS] : 8;
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int64_t k0 = (int64_t)b * BLOCK_COLS + 32 * s + 8 * q;
+            fetch<BT>(B, n, k0, (int)min((int64_t)8, W.K - k0), a.b[s]);
+        }
+    };
+    f32x4 acc = {0, 0, 0, 0};
+    auto use = [&](const asked &a) {
+        if constexpr (BT == SPMM_I8) {
+            u32x2 w[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) w[s] = weights_i8(a.word[s], a.zero[s / PER_GROUP] * 0x01010101u);
+            i32x4 part;
+#pragma unroll
+            for (int s = 0; s < 4; s += PER_GROUP == 1 ? 1 : 2) {
+                const bool begins = s % PER_GROUP == 0;
+                if constexpr (PER_GROUP == 1) {
+                    part = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, a.b[s].part[0]), __builtin_bit_cast(long, w[s]), i32x4{0, 0, 0, 0}, 0, 0, 0);
+                } else {
+                    const i32x4 x = {(int)a.b[s].part[0][0], (int)a.b[s].part[0][1], (int)a.b[s + 1].part[0][0], (int)a.b[s + 1].part[0][1]};
+                    const i32x4 y = {(int)w[s][0], (int)w[s][1], (int)w[s + 1][0], (int)w[s + 1][1]};
+                    part = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, begins ? i32x4{0, 0, 0, 0} : part, 0, 0, 0);
+                }
+                if (PER_GROUP < 4 || s == 2) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i] += a.scale[s / PER_GROUP] * (float)part[i];
+                }
+            }
+        } else {
+            f32x4 part;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if (s % PER_GROUP == 0) part = f32x4{0, 0, 0, 0};
+                if constexpr (BT == SPMM_F16) {
+                    part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.b[s].part[0]), weights_f16(a.word[s], a.zero[s / PER_GROUP]), part, 0, 0, 0);
+                } else {
+                    const bf16x8 w = weights_bf16(a.word[s], a.zero[s / PER_GROUP]);
+#pragma unroll
+                    for (int p = PARTS<BT> - 1; p >= 0; --p) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.b[s].part[p]), w, part, 0, 0, 0);
+                }
+                if (s % PER_GROUP == PER_GROUP - 1) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i] += a.scale[s / PER_GROUP] * part[i];
+                }
+            }
+        }
+    };
+    asked ring[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (first + i < last) ask(first + i, ring[i]);
+    for (int b = first; b < last; b += AHEAD) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (b + i >= last) break;
+            use(ring[i]);
+            if (b + i + AHEAD < last) ask(b + i + AHEAD, ring[i]);
+        }
+    }
+    *reinterpret_cast<f32x4 *>(&sums[wave][lane * 4]) = acc;
+    __syncthreads();
+    // the waves' sums, in wave order: a thread an element of C
+    if (threadIdx.x >= 256) return;
+    const int e = threadIdx.x, m = C.by_token ? e % 16 : e / 16, t = C.by_token ? e / 16 : e % 16;
+    const int64_t row = row_tile * TILE_ROWS + m;
+    if (row >= W.M || t >= N) return;
+    const int at = (t >> 2) * 64 + m * 4 + (t & 3);
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < KWAVES; ++w) v += sums[w][at];
+    if (BT == SPMM_I8) v *= B_scales[t];
+    store_as(C.data, C.by_token ? t * C.ld + row : row * C.ld + t, C.type, v);
+}
+
+template <int BT> hipError_t execute_few(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
+{
+    auto run = [&](auto per_group) {
+        constexpr int PER_GROUP = decltype(per_group)::value;
+        return launch_kernel(few_kernel<BT, PER_GROUP, 8>, dim3((unsigned)w.tiles), 512, 0, stream, w, B, B_scales, (int32_t)N, C);
+    };
+    if (w.group == 32) return run(std::integral_constant<int, 1>());
+    if (w.group == 64) return run(std::integral_constant<int, 2>());
+    return run(std::integral_constant<int, 4>());
+}
+
 template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, char *workspace, hipStream_t stream)
 {
+    if (N <= 16) return execute_few<BT>(w, B, B_scales, N, C, stream);
     const int64_t token_tiles = (N + 15) / 16;
     // a launch of each for 2^16 - 1 tiles of tokens at a time
     constexpr int64_t MOST = 65535 / 8 * 8;
@@ -250,8 +410,7 @@ template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, con
             constexpr int NT = decltype(nt)::value;
             return launch_kernel(product_kernel<BT, NT>, dim3((unsigned)w.tiles, (unsigned)((tiles + NT - 1) / NT)), 64 * WAVES, 0, stream, w, (const char *)workspace, scales, n, c);
         };
-        if (tiles == 1) e = product(std::integral_constant<int, 1>());
-        else if (tiles == 2) e = product(std::integral_constant<int, 2>());
+        if (tiles <= 2) e = product(std::integral_constant<int, 2>());
         else if (tiles <= 4) e = product(std::integral_constant<int, 4>());
         else e = product(std::integral_constant<int, 8>());
         if (e != hipSuccess) return e;
@@ -263,6 +422,7 @@ template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, con
 
 int64_t quant_workspace(const quant_matrix &w, int32_t type, int64_t N)
 {
+    if (N <= 16) return 0;
     const int64_t step = type == SPMM_F32 ? 3 * 1024 : type == SPMM_I8 ? 512 : 1024, tiles = (N + 15) / 16;
     const int64_t most = 65535 / 8 * 8;
     return (tiles < most ? tiles : most) * w.blocks * 4 * step;
