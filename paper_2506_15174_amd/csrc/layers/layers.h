@@ -18,8 +18,9 @@ namespace layers {
 // the neighbours 2 i and 2 i + 1 in the low halves of a 32-bit word, as 16-bit operands are held.
 //
 // Scales and zero points are [tile][group][TILE_ROWS].  Rows past M have scale 0, columns past K the code of their
-// group's zero point, so that they are whole numbers of 0.
-constexpr int TILE_ROWS = 16, BLOCK_COLS = 128, BLOCK_WORDS = TILE_ROWS * BLOCK_COLS / 8;
+// group's zero point, so that they are whole numbers of 0.  Memory is there for whole TILES_OF tiles, rows past M as above: a wave may have
+// that many.
+constexpr int TILE_ROWS = 16, BLOCK_COLS = 128, BLOCK_WORDS = TILE_ROWS * BLOCK_COLS / 8, TILES_OF = 4;
 constexpr int NIBBLE_COLUMN[8] = {0, 2, 4, 6, 1, 3, 5, 7};
 
 struct quant_matrix {

@@ -149,7 +149,7 @@ spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, c
     }
     hipError_t e = hipGetDevice(&p->device);
     if (e != hipSuccess) return status_of(e);
-    const int64_t code_bytes = (int64_t)w.tiles * w.blocks * BLOCK_WORDS * 4, padded = (int64_t)w.tiles * w.groups * TILE_ROWS;
+    const int64_t tiles = up_to(w.tiles, TILES_OF), code_bytes = tiles * w.blocks * BLOCK_WORDS * 4, padded = tiles * w.groups * TILE_ROWS;
     const int64_t scales_at = up_to(code_bytes, 256), zeros_at = scales_at + up_to(padded * 4, 256);
     p->bytes = zeros_at + (zeros ? up_to(padded, 256) : 0);
     if (code_bytes > 0) {
@@ -159,12 +159,11 @@ spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, c
         uint8_t *out_zeros = zeros ? reinterpret_cast<uint8_t *>(host.get() + zeros_at) : nullptr;
         // a thread for each MiB of codes, at most 16 and at most the machine's
         const int64_t most = std::max<int64_t>(1, std::min<int64_t>(16, std::thread::hardware_concurrency()));
-        const int64_t threads = std::min<int64_t>(std::min(most, (int64_t)w.tiles), std::max<int64_t>(1, code_bytes >> 20));
+        const int64_t threads = std::min<int64_t>(std::min(most, tiles), std::max<int64_t>(1, code_bytes >> 20));
         std::vector<std::thread> others;
         others.reserve((size_t)threads);
-        int64_t done = 0;
         for (int64_t t = 0; t < threads; ++t) {
-            const int64_t t0 = w.tiles * t / threads, t1 = w.tiles * (t + 1) / threads;
+            const int64_t t0 = tiles * t / threads, t1 = tiles * (t + 1) / threads;
             auto work = [=, &w] { lay_out(w, t0, t1, codes, scales, zeros, out_codes, out_scales, out_zeros); };
             if (t + 1 == threads) {
                 work();
@@ -175,10 +174,8 @@ spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, c
                     work();
                 }
             }
-            done = t1;
         }
         for (std::thread &t : others) t.join();
-        if (done != w.tiles) return SPMM_ERR_ALLOC;
         e = hipMalloc(reinterpret_cast<void **>(&p->memory), (size_t)p->bytes);
         if (e != hipSuccess) {
             (void)hipGetLastError();

@@ -39,9 +39,60 @@ constexpr int WAVES = 8;
 //
 // [token tile of 16][block of 128 columns][step of 32][part][lane][8 columns], 16 bytes a lane for 16-bit elements;
 // codes hold two steps in the 16 bytes of a lane: [token tile][block][pair of steps][lane][step][8 columns].
-// Lane 16 q + t holds token t, columns 32 s + 8 q + j.  Tokens and columns that do not exist are zeros.
+// Lane 16 q + t holds token t, columns 32 s + 8 q + j.  Columns that do not exist are zeros.
 
-// Eight columns of a token as operands: a part each; codes are eight bytes.
+// Eight columns of a token, as they are read.
+template <int BT> struct raw {
+    u32x4 v;
+};
+template <> struct raw<SPMM_F32> {
+    float v[8];
+};
+template <> struct raw<SPMM_I8> {
+    u32x2 v;
+};
+
+template <int BT> struct stored {
+    typedef uint16_t type;
+};
+template <> struct stored<SPMM_F32> {
+    typedef float type;
+};
+template <> struct stored<SPMM_I8> {
+    typedef uint8_t type;
+};
+
+// Columns k0 .. k0 + 7 of a token whose column 0 lies at `base`; `ld` bytes from one column to the next where a row of memory is a feature.
+// TAIL: of columns 0 .. `left` - 1 only; the others are 0 (and read at the last one's place).
+template <int BT, bool BY_TOKEN, bool TAIL> __device__ inline raw<BT> fetch(const char *base, int64_t ld, int k0, int left)
+{
+    typedef typename stored<BT>::type T;
+    raw<BT> o;
+    T x[8];
+    if constexpr (BY_TOKEN && !TAIL) {
+        const neighbours<T, 8> n = *reinterpret_cast<const neighbours<T, 8> *>(base + k0 * (int)sizeof(T));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = n.v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = TAIL ? min(k0 + j, left - 1) : k0 + j;
+            x[j] = *reinterpret_cast<const T *>(base + k * (BY_TOKEN ? (int64_t)sizeof(T) : ld));
+            if (TAIL && k0 + j >= left) x[j] = 0;
+        }
+    }
+    if constexpr (BT == SPMM_F32) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o.v[j] = x[j];
+    } else {
+        constexpr int EACH = 4 / (int)sizeof(T);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o.v[j / EACH] = (j % EACH ? o.v[j / EACH] : 0u) | (uint32_t)x[j] << (32 / EACH * (j % EACH));
+    }
+    return o;
+}
+
+// The same as operands of matrix instructions, a part each; codes are eight bytes.
 template <int BT> struct operands {
     u32x4 part[PARTS<BT>];
 };
@@ -49,76 +100,64 @@ template <> struct operands<SPMM_I8> {
     u32x2 part[1];
 };
 
-// fp32: each part is the upper half of what is left, cut off, not rounded, so that large values stay finite.  An infinity or a NaN is the first
-// part's alone.
-__device__ inline void split(const float (&v)[8], operands<SPMM_F32> &o)
+// A value in a register of its own.  Without this the compiler (ROCm 7.2) gave operands made of a wide load's words the load's own registers and wrote the first
+// before it read the last: v18 = perm(v39, v38), then v20 = perm(v19, v18), where v18 to v21 held the words 4 to 7.
+__device__ inline uint32_t apart(uint32_t v)
 {
-#pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-        uint32_t bits[2][3];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float x = v[j + h];
-            const bool finite = __builtin_isfinite(x);
-            const uint32_t b0 = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
-            const float left1 = x - __builtin_bit_cast(float, b0);
-            const uint32_t b1 = __builtin_bit_cast(uint32_t, left1) & 0xffff0000u;
-            const float left2 = left1 - __builtin_bit_cast(float, b1);
-            bits[h][0] = x != x ? 0x7fc00000u : b0;
-            bits[h][1] = finite ? b1 : 0;
-            bits[h][2] = finite ? __builtin_bit_cast(uint32_t, left2) : 0;
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) o.part[p][j / 2] = __builtin_amdgcn_perm(bits[1][p], bits[0][p], 0x07060302u);
-    }
+    asm("" : "+v"(v));
+    return v;
 }
 
-// Columns k0 .. k0 + 7 of token n, of which `there` exist (the others are 0).
-template <int BT> __device__ inline void fetch(const tensor &B, int64_t n, int64_t k0, int there, operands<BT> &o)
+template <int BT> __device__ inline operands<BT> operands_of(const raw<BT> &x)
 {
-    const int64_t stride = B.by_token ? 1 : B.ld, at = B.by_token ? n * B.ld + k0 : k0 * B.ld + n;
+    operands<BT> o;
     if constexpr (BT == SPMM_I8) {
-        u32x2 raw = {0, 0};  // (codes lie one token a row)
-        if (there >= 8) {
-            raw = __builtin_bit_cast(u32x2, *reinterpret_cast<const neighbours<int8_t, 8> *>(B.data + at));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < there) raw[j / 4] |= (uint32_t) reinterpret_cast<const uint8_t *>(B.data)[at + j] << (8 * (j % 4));
-        }
         // the order in which the weights' nibbles become bytes: 0 4 1 5, 2 6 3 7
-        o.part[0] = u32x2{__builtin_amdgcn_perm(raw[1], raw[0], 0x05010400u), __builtin_amdgcn_perm(raw[1], raw[0], 0x07030602u)};
+        const uint32_t low = apart(x.v[0]), high = apart(x.v[1]);
+        o.part[0] = u32x2{__builtin_amdgcn_perm(high, low, 0x05010400u), __builtin_amdgcn_perm(high, low, 0x07030602u)};
     } else if constexpr (BT == SPMM_F32) {
-        float v[8];
-        if (B.by_token) {
-            load_row<float>(B.data, at, there, v);
-        } else {
+        // Each part is the upper half of what is left: cut off, not rounded, so that large values stay finite.
+        uint32_t first[8], second[8], third[8], largest = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < there ? reinterpret_cast<const float *>(B.data)[at + j * stride] : 0.0f;
+        for (int j = 0; j < 8; ++j) {
+            first[j] = apart(__builtin_bit_cast(uint32_t, x.v[j]));
+            largest = max(largest, first[j] & 0x7fffffffu);
+            const float left = x.v[j] - __builtin_bit_cast(float, first[j] & 0xffff0000u);
+            second[j] = __builtin_bit_cast(uint32_t, left);
+            third[j] = __builtin_bit_cast(uint32_t, left - __builtin_bit_cast(float, second[j] & 0xffff0000u));
         }
-        split(v, o);
-    } else {
-        if (B.by_token && there >= 8) {
-            o.part[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const neighbours<uint16_t, 8> *>(B.data + 2 * at));
-        } else {
-            u32x4 word = {0, 0, 0, 0};
+        if (largest >= 0x7f800000u) {  // an infinity or a NaN is the first part's alone
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t v = j < there ? reinterpret_cast<const uint16_t *>(B.data)[at + j * stride] : 0;
-                word[j / 2] |= v << (16 * (j & 1));
+                const uint32_t magnitude = first[j] & 0x7fffffffu;
+                first[j] = magnitude > 0x7f800000u ? 0x7fc00000u : first[j];
+                second[j] = magnitude >= 0x7f800000u ? 0 : second[j];
+                third[j] = magnitude >= 0x7f800000u ? 0 : third[j];
             }
-            o.part[0] = word;
         }
+        auto upper = [](const uint32_t (&v)[8]) {
+            constexpr uint32_t HALVES = 0x07060302u;
+            return u32x4{__builtin_amdgcn_perm(v[1], v[0], HALVES), __builtin_amdgcn_perm(v[3], v[2], HALVES), __builtin_amdgcn_perm(v[5], v[4], HALVES),
+                         __builtin_amdgcn_perm(v[7], v[6], HALVES)};
+        };
+        o.part[0] = upper(first), o.part[1] = upper(second), o.part[2] = upper(third);
+    } else {
+        o.part[0] = x.v;
     }
+    return o;
 }
 
-template <int BT> __global__ __launch_bounds__(256) void pack_kernel(tensor B, int64_t K, int64_t N, int32_t blocks, char *out)
+template <int BT, bool BY_TOKEN> __global__ __launch_bounds__(256) void pack_kernel(tensor B, int64_t K, int64_t N, int32_t blocks, char *out)
 {
+    constexpr int64_t SIZE = sizeof(typename stored<BT>::type);
     const int lane = threadIdx.x & 63, s = threadIdx.x >> 6, t = lane & 15, q = lane >> 4;
-    const int64_t block = blockIdx.x, tile = blockIdx.y, n = tile * 16 + t, k0 = block * BLOCK_COLS + 32 * s + 8 * q;
+    const int64_t block = blockIdx.x, tile = blockIdx.y, n = tile * 16 + t;
     char *block_out = out + (tile * blocks + block) * (4 * PARTS<BT> * STEP_BYTES<BT>);
-    operands<BT> o;
-    fetch<BT>(B, n, k0, n < N ? (int)min((int64_t)8, K - k0) : 0, o);
+    const int left = (int)min((int64_t)BLOCK_COLS, K - block * BLOCK_COLS);
+    // tokens that do not exist: the last one's (what they give is not stored)
+    const char *base = B.data + (min(n, N - 1) * (BY_TOKEN ? B.ld : 1) + block * BLOCK_COLS * (BY_TOKEN ? 1 : B.ld)) * SIZE;
+    const operands<BT> o = operands_of<BT>(left == BLOCK_COLS ? fetch<BT, BY_TOKEN, false>(base, B.ld * SIZE, 32 * s + 8 * q, left) :
+                                                                fetch<BT, BY_TOKEN, true>(base, B.ld * SIZE, 32 * s + 8 * q, left));
     if constexpr (BT == SPMM_I8) {
         *reinterpret_cast<u32x2 *>(block_out + (s >> 1) * 1024 + lane * 16 + (s & 1) * 8) = o.part[0];
     } else {
@@ -153,6 +192,18 @@ __device__ inline bf16x8 weights_bf16(uint32_t w, int zero)
         v[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, high), __builtin_bit_cast(uint32_t, low), 0x07060302u);
     }
     return __builtin_bit_cast(bf16x8, v);
+}
+
+// The same in fp32, two steps of the same.
+__device__ inline void weights_f32(uint32_t w, int zero, float (&v)[8])
+{
+    const float low_base = 8388608.0f + (float)zero, high_base = 128.0f + (float)zero;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t t = w >> (4 * i);
+        v[2 * i] = __builtin_bit_cast(float, (t & 0xfu) | 0x4b000000u) - low_base;
+        v[2 * i + 1] = __builtin_bit_cast(float, (t & 0xf0000u) | 0x43000000u) - high_base;
+    }
 }
 
 // The same in bytes, columns in the order 0 4 1 5, 2 6 3 7: no borrow leaves a byte that has 128 added.
@@ -278,121 +329,184 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
 // Up to 16 tokens are one tile, and a product is over in the time of a few memory accesses: one launch, in which every wave reads its columns of
 // B as it reads its weights and makes operands of them itself.  Lanes of tokens that do not exist read the last one's (an access the
 // wave makes anyway); their results are not stored.  Weights, scales and B of AHEAD blocks are asked for before the first is used.
-// PER_GROUP: steps of 32 columns behind which a group's sum is full (4, 2 or 1).
+//   PER_GROUP  steps of 32 columns behind which a group's sum is full (4, 2 or 1)
+//   RT         tiles of rows of a wave, which share its operands of B
+//   FMA        one token in fp32 is multiplied by ordinary instructions, a lane a row and a quarter of the columns: making three parts of a value
+//              takes six
+//   KWAVES     waves of a workgroup, which share K
 
-template <int BT, int PER_GROUP, int KWAVES> __global__ __launch_bounds__(64 * KWAVES) void few_kernel(quant_matrix W, tensor B, const float *B_scales, int32_t N, tensor C)
+template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, bool FMA> __global__ __launch_bounds__(64 * KWAVES) void few_kernel(quant_matrix W, tensor B, const float *B_scales, int32_t N, tensor C)
 {
-    __shared__ float sums[KWAVES][256];
-    constexpr int AHEAD = BT == SPMM_F32 ? 1 : 2, SUMS = 4 / PER_GROUP;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4, n = min(r, N - 1);
-    const int64_t row_tile = blockIdx.x;
+    __shared__ float sums[KWAVES][RT][256];
+    constexpr int SUMS = 4 / PER_GROUP;
+    constexpr int64_t SIZE = sizeof(typename stored<BT>::type);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
     const int group_blocks = PER_GROUP < 4 ? 1 : (int)(W.group / BLOCK_COLS);
-    const uint32_t *codes = W.codes + row_tile * W.blocks * BLOCK_WORDS + lane * 4;
-    const float *scales = W.scales + row_tile * W.groups * TILE_ROWS + r;
-    const uint8_t *zeros = W.zeros ? W.zeros + row_tile * W.groups * TILE_ROWS + r : nullptr;
     const int first = (int)((int64_t)W.blocks * wave / KWAVES), last = (int)((int64_t)W.blocks * (wave + 1) / KWAVES);
+    // (the plan's memory has whole fours of row tiles)
+    const int64_t tile0 = (int64_t)blockIdx.x * RT;
+    const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
+    const float *const scales = W.scales + tile0 * W.groups * TILE_ROWS;
+    const uint8_t *const zeros = W.zeros ? W.zeros + tile0 * W.groups * TILE_ROWS : nullptr;
+    const int64_t column = (BY_TOKEN ? 1 : B.ld) * SIZE;  // bytes from one to the next
+    const char *const token = B.data + (FMA ? 0 : min(r, N - 1)) * (BY_TOKEN ? B.ld : 1) * SIZE, *const mine = token + 8 * q * column;
     struct asked {
-        u32x4 word;
-        float scale[SUMS];
-        int zero[SUMS];
-        operands<BT> b[4];
+        u32x4 word[RT];
+        float scale[RT][SUMS];
+        int zero[RT][SUMS];
+        raw<BT> b[4];
     };
-    auto ask = [&](int b, asked &a) {
-        a.word = *reinterpret_cast<const u32x4 *>(codes + (int64_t)b * BLOCK_WORDS);
+    auto ask = [&](int b, asked &a, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
 #pragma unroll
-        for (int g = 0; g < SUMS; ++g) {
-            const int group = PER_GROUP < 4 ? min(W.groups - 1, b * SUMS + g) : b / group_blocks;
-            a.scale[g] = scales[group * TILE_ROWS];
-            a.zero[g] = zeros ? zeros[group * TILE_ROWS] : 8;
-        }
+        for (int i = 0; i < RT; ++i) a.word[i] = reinterpret_cast<const u32x4 *>(codes + ((int64_t)i * W.blocks + b) * BLOCK_WORDS)[lane];
+        const int left = (int)(W.K - (int64_t)b * BLOCK_COLS);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int64_t k0 = (int64_t)b * BLOCK_COLS + 32 * s + 8 * q;
-            fetch<BT>(B, n, k0, (int)min((int64_t)8, W.K - k0), a.b[s]);
+        for (int s = 0; s < 4; ++s) a.b[s] = fetch<BT, BY_TOKEN, TAIL>((TAIL ? token : mine) + b * BLOCK_COLS * column, column, 32 * s + (TAIL ? 8 * q : 0), left);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+#pragma unroll
+            for (int g = 0; g < SUMS; ++g) {
+                const int64_t group = (int64_t)i * W.groups + (PER_GROUP < 4 ? min(W.groups - 1, b * SUMS + g) : b / group_blocks);
+                a.scale[i][g] = (scales + group * TILE_ROWS)[r];
+                a.zero[i][g] = zeros ? (zeros + group * TILE_ROWS)[r] : 8;
+            }
         }
     };
-    f32x4 acc = {0, 0, 0, 0};
+    f32x4 acc[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i] = f32x4{0, 0, 0, 0};
     auto use = [&](const asked &a) {
-        if constexpr (BT == SPMM_I8) {
-            u32x2 w[4];
+        operands<BT> o[4];
+        if constexpr (!FMA) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) w[s] = weights_i8(a.word[s], a.zero[s / PER_GROUP] * 0x01010101u);
-            i32x4 part;
+            for (int s = 0; s < 4; ++s) o[s] = operands_of<BT>(a.b[s]);
+        }
 #pragma unroll
-            for (int s = 0; s < 4; s += PER_GROUP == 1 ? 1 : 2) {
-                const bool begins = s % PER_GROUP == 0;
-                if constexpr (PER_GROUP == 1) {
-                    part = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, a.b[s].part[0]), __builtin_bit_cast(long, w[s]), i32x4{0, 0, 0, 0}, 0, 0, 0);
-                } else {
-                    const i32x4 x = {(int)a.b[s].part[0][0], (int)a.b[s].part[0][1], (int)a.b[s + 1].part[0][0], (int)a.b[s + 1].part[0][1]};
-                    const i32x4 y = {(int)w[s][0], (int)w[s][1], (int)w[s + 1][0], (int)w[s + 1][1]};
-                    part = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, begins ? i32x4{0, 0, 0, 0} : part, 0, 0, 0);
+        for (int i = 0; i < RT; ++i) {
+            if constexpr (FMA) {
+                float part = 0.0f;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    float w[8];
+                    weights_f32(a.word[i][s], a.zero[i][s / PER_GROUP], w);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) part = __builtin_fmaf(w[j], a.b[s].v[j], part);
+                    if (s % PER_GROUP == PER_GROUP - 1) acc[i][0] += a.scale[i][s / PER_GROUP] * part, part = 0.0f;
                 }
-                if (PER_GROUP < 4 || s == 2) {
+            } else if constexpr (BT == SPMM_I8) {
+                u32x2 w[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i] += a.scale[s / PER_GROUP] * (float)part[i];
+                for (int s = 0; s < 4; ++s) w[s] = weights_i8(a.word[i][s], a.zero[i][s / PER_GROUP] * 0x01010101u);
+                i32x4 part;
+#pragma unroll
+                for (int s = 0; s < 4; s += PER_GROUP == 1 ? 1 : 2) {
+                    const bool begins = s % PER_GROUP == 0;
+                    if constexpr (PER_GROUP == 1) {
+                        part = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, o[s].part[0]), __builtin_bit_cast(long, w[s]), i32x4{0, 0, 0, 0}, 0, 0, 0);
+                    } else {
+                        const i32x4 x = {(int)o[s].part[0][0], (int)o[s].part[0][1], (int)o[s + 1].part[0][0], (int)o[s + 1].part[0][1]};
+                        const i32x4 y = {(int)w[s][0], (int)w[s][1], (int)w[s + 1][0], (int)w[s + 1][1]};
+                        part = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, begins ? i32x4{0, 0, 0, 0} : part, 0, 0, 0);
+                    }
+                    if (PER_GROUP < 4 || s == 2) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][e] += a.scale[i][s / PER_GROUP] * (float)part[e];
+                    }
                 }
-            }
-        } else {
-            f32x4 part;
+            } else {
+                f32x4 part;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if (s % PER_GROUP == 0) part = f32x4{0, 0, 0, 0};
-                if constexpr (BT == SPMM_F16) {
-                    part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.b[s].part[0]), weights_f16(a.word[s], a.zero[s / PER_GROUP]), part, 0, 0, 0);
-                } else {
-                    const bf16x8 w = weights_bf16(a.word[s], a.zero[s / PER_GROUP]);
+                for (int s = 0; s < 4; ++s) {
+                    if (s % PER_GROUP == 0) part = f32x4{0, 0, 0, 0};
+                    if constexpr (BT == SPMM_F16) {
+                        part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, o[s].part[0]), weights_f16(a.word[i][s], a.zero[i][s / PER_GROUP]), part, 0, 0, 0);
+                    } else {
+                        const bf16x8 w = weights_bf16(a.word[i][s], a.zero[i][s / PER_GROUP]);
 #pragma unroll
-                    for (int p = PARTS<BT> - 1; p >= 0; --p) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.b[s].part[p]), w, part, 0, 0, 0);
-                }
-                if (s % PER_GROUP == PER_GROUP - 1) {
+                        for (int p = PARTS<BT> - 1; p >= 0; --p) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o[s].part[p]), w, part, 0, 0, 0);
+                    }
+                    if (s % PER_GROUP == PER_GROUP - 1) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i] += a.scale[s / PER_GROUP] * part[i];
+                        for (int e = 0; e < 4; ++e) acc[i][e] += a.scale[i][s / PER_GROUP] * part[e];
+                    }
                 }
             }
         }
     };
+    // The last block of a K that is no multiple of 128 comes by itself.
+    const int whole = min(last, (int)(W.K / BLOCK_COLS));
     asked ring[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
-        if (first + i < last) ask(first + i, ring[i]);
-    for (int b = first; b < last; b += AHEAD) {
+        if (first + i < whole) ask(first + i, ring[i], std::false_type());
+    for (int b = first; b < whole; b += AHEAD) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            if (b + i >= last) break;
+            if (b + i >= whole) break;
             use(ring[i]);
-            if (b + i + AHEAD < last) ask(b + i + AHEAD, ring[i]);
+            if (b + i + AHEAD < whole) ask(b + i + AHEAD, ring[i], std::false_type());
         }
     }
-    *reinterpret_cast<f32x4 *>(&sums[wave][lane * 4]) = acc;
+    if (whole < last) {
+        ask(whole, ring[0], std::true_type());
+        use(ring[0]);
+    }
+    if constexpr (FMA) {  // the four quarters of the columns
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            acc[i][0] += __shfl_xor(acc[i][0], 16);
+            acc[i][0] += __shfl_xor(acc[i][0], 32);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4 *>(&sums[wave][i][lane * 4]) = acc[i];
     __syncthreads();
     // the waves' sums, in wave order: a thread an element of C
-    if (threadIdx.x >= 256) return;
-    const int e = threadIdx.x, m = C.by_token ? e % 16 : e / 16, t = C.by_token ? e / 16 : e % 16;
-    const int64_t row = row_tile * TILE_ROWS + m;
-    if (row >= W.M || t >= N) return;
-    const int at = (t >> 2) * 64 + m * 4 + (t & 3);
-    float v = 0.0f;
+    for (int e = threadIdx.x; e < RT * 256; e += 64 * KWAVES) {
+        const int m = C.by_token ? e % (16 * RT) : e / 16, t = C.by_token ? e / (16 * RT) : e % 16;
+        const int64_t row = tile0 * TILE_ROWS + m;
+        if (row >= W.M || t >= N) continue;
+        const int at = (t >> 2) * 64 + (m % 16) * 4 + (t & 3);
+        float v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < KWAVES; ++w) v += sums[w][at];
-    if (BT == SPMM_I8) v *= B_scales[t];
-    store_as(C.data, C.by_token ? t * C.ld + row : row * C.ld + t, C.type, v);
+        for (int w = 0; w < KWAVES; ++w) v += sums[w][m / 16][at];
+        if (BT == SPMM_I8) v *= B_scales[t];
+        store_as(C.data, C.by_token ? t * C.ld + row : row * C.ld + t, C.type, v);
+    }
 }
 
-template <int BT> hipError_t execute_few(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
+template <int V> using constant = std::integral_constant<int, V>;
+
+template <int BT, bool BY_TOKEN, bool FMA> hipError_t execute_few(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
-    auto run = [&](auto per_group) {
-        constexpr int PER_GROUP = decltype(per_group)::value;
-        return launch_kernel(few_kernel<BT, PER_GROUP, 8>, dim3((unsigned)w.tiles), 512, 0, stream, w, B, B_scales, (int32_t)N, C);
+    auto shaped = [&](auto per_group, auto rt, auto kwaves, auto ahead) {
+        constexpr int PER_GROUP = decltype(per_group)::value, RT = decltype(rt)::value, KWAVES = decltype(kwaves)::value, AHEAD = decltype(ahead)::value;
+        return launch_kernel(few_kernel<BT, BY_TOKEN, PER_GROUP, RT, KWAVES, AHEAD, FMA>, dim3((unsigned)((w.tiles + RT - 1) / RT)), 64 * KWAVES, 0, stream, w, B, B_scales,
+                             (int32_t)N, C);
     };
-    if (w.group == 32) return run(std::integral_constant<int, 1>());
-    if (w.group == 64) return run(std::integral_constant<int, 2>());
-    return run(std::integral_constant<int, 4>());
+    auto run = [&](auto per_group) {
+        // (what the registers hold)
+        constexpr int AHEAD = BT == SPMM_F32 && !FMA ? 1 : 2, LESS = decltype(per_group)::value < 4 ? 1 : AHEAD;
+        if (w.tiles >= 1024) return shaped(per_group, constant<4>(), constant<8>(), constant<LESS>());
+        if (w.tiles >= 512) return shaped(per_group, constant<2>(), constant<8>(), constant<AHEAD>());
+        if constexpr (BY_TOKEN && BT != SPMM_F32)
+            if (w.blocks > 8) return shaped(per_group, constant<1>(), constant<16>(), constant<LESS>());
+        return shaped(per_group, constant<1>(), constant<8>(), constant<1>());
+    };
+    if (w.group == 32) return run(constant<1>());
+    if (w.group == 64) return run(constant<2>());
+    return run(constant<4>());
 }
 
 template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, char *workspace, hipStream_t stream)
 {
-    if (N <= 16) return execute_few<BT>(w, B, B_scales, N, C, stream);
+    if (N <= 16) {
+        if constexpr (BT == SPMM_F32)
+            if (B.by_token && N == 1) return execute_few<BT, true, true>(w, B, B_scales, N, C, stream);
+        if (B.by_token) return execute_few<BT, true, false>(w, B, B_scales, N, C, stream);
+        if constexpr (BT != SPMM_I8) return execute_few<BT, false, false>(w, B, B_scales, N, C, stream);
+    }
     const int64_t token_tiles = (N + 15) / 16;
     // a launch of each for 2^16 - 1 tiles of tokens at a time
     constexpr int64_t MOST = 65535 / 8 * 8;
@@ -404,7 +518,9 @@ template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, con
         c.data += n0 * (C.by_token ? C.ld : 1) * c_size;
         const float *scales = B_scales ? B_scales + n0 : nullptr;
         hipError_t e = hipSuccess;
-        if (w.blocks > 0) e = launch_kernel(pack_kernel<BT>, dim3((unsigned)w.blocks, (unsigned)tiles), 256, 0, stream, b, w.K, n, w.blocks, workspace);
+        const dim3 grid((unsigned)w.blocks, (unsigned)tiles);
+        if (w.blocks > 0 && b.by_token) e = launch_kernel(pack_kernel<BT, true>, grid, 256, 0, stream, b, w.K, n, w.blocks, workspace);
+        else if (w.blocks > 0) e = launch_kernel(pack_kernel<BT, false>, grid, 256, 0, stream, b, w.K, n, w.blocks, workspace);
         if (e != hipSuccess) return e;
         auto product = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;

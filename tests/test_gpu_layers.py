@@ -71,6 +71,17 @@ def test_whole_numbers_are_exact(type, group, N):
 
 
 @pytest.mark.parametrize("type", FLOATS + ("int8",))
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,K", [(8200, 520), (16500, 260), (70, 2200), (8200, 2200), (16500, 1290)])
+def test_whole_numbers_are_exact_in_every_shape_of_workgroup(type, group, M, K):
+    """Rows and columns for which waves have one, two or four tiles of rows, and one or several blocks of columns."""
+    for N in (1, 2, 7, 16, 33, 100):
+        check_product(M, K, N, group, type, "tokens", N + group, whole=True)
+        if type != "int8":
+            check_product(M, K, N, group, type, "features", N + group + 1, whole=True)
+
+
+@pytest.mark.parametrize("type", FLOATS + ("int8",))
 @pytest.mark.parametrize("M,K,N,group", [(1, 1, 1, 32), (1, 1, 5, 64), (5, 2, 1, 128), (16, 128, 16, 32), (17, 33, 2, 32), (33, 129, 33, 128), (64, 65, 64, 64),
                                          (100, 1000, 1, 128), (300, 257, 129, 384), (31, 4100, 7, 128), (48, 640, 300, 1024), (2100, 96, 8, 64), (130, 2048, 513, 64)])
 def test_odd_sizes(type, M, K, N, group):
