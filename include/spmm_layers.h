@@ -50,7 +50,7 @@ typedef struct spmm_quant spmm_quant_t; /* opaque */
  *           a row is shorter where K is not a multiple
  *   codes   HOST  uint8[M * ceil(K / 2)]: two codes of 0..15 a byte, that of the even column in the low half; rows
  *                 start at a byte, the high half of a row's last byte is not looked at where K is odd
- *   scales  HOST  float[M * ceil(K / group)], finite (else SPMM_ERR_INVALID_ARG)
+ *   scales  HOST  float[M * ceil(K / group)], magnitudes up to 2^120 (else SPMM_ERR_INVALID_ARG)
  *   zeros   HOST  uint8[M * ceil(K / group)], each in 0..15 (else SPMM_ERR_INVALID_ARG), or NULL: 8 everywhere
  *
  * The arrays are only read during the call.  The plan owns its device memory on the device that is current at the
@@ -85,8 +85,8 @@ spmm_status_t spmm_quant_workspace(const spmm_quant_t *plan, int32_t B_type, int
  *            content before the call does not matter
  * Sums are held in 32 bits: weights enter as whole numbers (code - zero), a sum of up to 128 of them, or of a group
  * if that is smaller, is exact in whole numbers for codes and accumulated in fp32 for floating B (fp32 B in three
- * bf16 parts that add up to it), then multiplied by the group's scale in fp32.  Values of an fp32 B below 2^-110 may
- * count as zero.
+ * bf16 parts that add up to it), then multiplied by the group's scale in fp32.  Values of B below 2^-100 may count as
+ * zero.
  */
 spmm_status_t spmm_quant_execute(const spmm_quant_t *plan, const spmm_tensor_t *B, const float *B_scales, int64_t N,
                                  const spmm_tensor_t *C, void *workspace, size_t workspace_bytes, void *stream);

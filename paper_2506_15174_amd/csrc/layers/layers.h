@@ -15,7 +15,7 @@ namespace layers {
 // codes of row r, word s of its four those of columns 32 s + 8 q + j, j = 0..7, of the block.  So one word is what a
 // lane hands to a matrix instruction of 32 columns, and the four words of a lane lie in one group of 128 columns, in
 // one of 64 two by two, in one of 32 each.  Inside a word nibble i holds j = NIBBLE_COLUMN[i]: a shift by 4 i and one mask give
-// the neighbours 2 i and 2 i + 1 in the low halves of a 32-bit word, as 16-bit operands are held.
+// the neighbours 2 i and 2 i + 1 in the low halves of a 32-bit word, as 16-bit operands are held.  A nibble is code - 8 in two's complement.
 //
 // Scales and zero points are [tile][group][TILE_ROWS].  Rows past M have scale 0, columns past K the code of their
 // group's zero point, so that they are whole numbers of 0.  Memory is there for whole TILES_OF tiles, rows past M as above: a wave may have

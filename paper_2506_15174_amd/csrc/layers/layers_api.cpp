@@ -34,6 +34,9 @@ constexpr int64_t MOST_EXTENT = INT32_MAX;
 // a launch has less than 2^32 threads along an axis: 32 for a row of weights, 2 for a column
 constexpr int64_t MOST_ROWS = (int64_t)1 << 26, MOST_COLS = (int64_t)1 << 30;
 
+// the kernels multiply scales by 16
+constexpr float MOST_SCALE = 0x1p120f;
+
 int64_t up_to(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
 int64_t parts_of(int64_t n, int64_t part) { return n / part + (n % part != 0); }
 
@@ -95,11 +98,11 @@ void lay_out(const quant_matrix &w, int64_t t0, int64_t t1, const uint8_t *codes
              uint8_t *out_zeros)
 {
     const int64_t row_bytes = parts_of(w.K, 2);
-    // the word of eight codes, four bytes as the caller has them (nibble i: column i), in the order of NIBBLE_COLUMN
+    // the word of eight codes, four bytes as the caller has them (nibble i: column i), in the order of NIBBLE_COLUMN and less 8
     auto ordered = [](uint32_t v) {
         uint32_t o = 0;
         for (int i = 0; i < 8; ++i) o |= ((v >> (4 * NIBBLE_COLUMN[i])) & 15u) << (4 * i);
-        return o;
+        return o ^ 0x88888888u;
     };
     for (int64_t tile = t0; tile < t1; ++tile) {
         for (int r = 0; r < TILE_ROWS; ++r) {
@@ -145,7 +148,7 @@ spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, c
     if (M > 0 && K > 0) {
         if (!codes || !scales) return SPMM_ERR_INVALID_ARG;
         for (int64_t i = 0; i < n_scales; ++i)
-            if (!std::isfinite(scales[i]) || (zeros && zeros[i] > 15)) return SPMM_ERR_INVALID_ARG;
+            if (!(std::fabs(scales[i]) <= MOST_SCALE) || (zeros && zeros[i] > 15)) return SPMM_ERR_INVALID_ARG;
     }
     hipError_t e = hipGetDevice(&p->device);
     if (e != hipSuccess) return status_of(e);

@@ -168,6 +168,8 @@ template <int BT, bool BY_TOKEN> __global__ __launch_bounds__(256) void pack_ker
 
 // ---- weights as the instructions take them -------------------------------------------------------------------
 
+// A nibble is code - 8 in two's complement: `zero` is the zero point.
+
 // code - zero of eight columns in f16: 1024 + code is a mask away (its last bit is worth 1), the difference is exact.
 __device__ inline f16x8 weights_f16(uint32_t w, int zero)
 {
@@ -175,49 +177,60 @@ __device__ inline f16x8 weights_f16(uint32_t w, int zero)
     const f16x2 base = {z, z};
     f16x2 v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u) - base;
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) ^ 0x64086408u) - base;
     return __builtin_bit_cast(f16x8, *reinterpret_cast<u32x4 *>(v));
 }
 
-// The same in bf16, by way of fp32: 2^23 + code and 128 + code are a mask away, the upper half of the exact difference is its bf16.
-__device__ inline bf16x8 weights_bf16(uint32_t w, int zero)
+// (code - 8) / 16 of the low nibble of byte I, which the hardware has an instruction for.
+template <int I> __device__ inline float sixteenths(uint32_t w)
 {
-    const float low_base = 8388608.0f + (float)zero, high_base = 128.0f + (float)zero;
-    u32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t t = w >> (4 * i);
-        const float low = __builtin_bit_cast(float, (t & 0xfu) | 0x4b000000u) - low_base;
-        const float high = __builtin_bit_cast(float, (t & 0xf0000u) | 0x43000000u) - high_base;
-        v[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, high), __builtin_bit_cast(uint32_t, low), 0x07060302u);
-    }
-    return __builtin_bit_cast(bf16x8, v);
+    float f;
+    if constexpr (I == 0) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(w));
+    if constexpr (I == 1) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(w));
+    if constexpr (I == 2) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(w));
+    if constexpr (I == 3) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(w));
+    return f;
 }
 
-// The same in fp32, two steps of the same.
-__device__ inline void weights_f32(uint32_t w, int zero, float (&v)[8])
+// (code - zero) / 16 of eight columns in fp32 (WEIGHT_UNIT makes up for the 16).  ZEROS: the plan has zero points, else they are 8.
+template <bool ZEROS> __device__ inline void weights_f32(uint32_t w, int zero, float (&v)[8])
 {
-    const float low_base = 8388608.0f + (float)zero, high_base = 128.0f + (float)zero;
+    const uint32_t odd = w >> 4;  // nibbles 0 2 4 6 are columns 0 4 1 5, the others 2 6 3 7
+    v[0] = sixteenths<0>(w), v[4] = sixteenths<1>(w), v[1] = sixteenths<2>(w), v[5] = sixteenths<3>(w);
+    v[2] = sixteenths<0>(odd), v[6] = sixteenths<1>(odd), v[3] = sixteenths<2>(odd), v[7] = sixteenths<3>(odd);
+    if constexpr (ZEROS) {
+        const float less = (float)(zero - 8) * 0.0625f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t t = w >> (4 * i);
-        v[2 * i] = __builtin_bit_cast(float, (t & 0xfu) | 0x4b000000u) - low_base;
-        v[2 * i + 1] = __builtin_bit_cast(float, (t & 0xf0000u) | 0x43000000u) - high_base;
+        for (int j = 0; j < 8; ++j) v[j] -= less;
     }
 }
 
-// The same in bytes, columns in the order 0 4 1 5, 2 6 3 7: no borrow leaves a byte that has 128 added.
+// The same in bf16: the upper half of the fp32, which holds it exactly.
+template <bool ZEROS> __device__ inline bf16x8 weights_bf16(uint32_t w, int zero)
+{
+    float v[8];
+    weights_f32<ZEROS>(w, zero, v);
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, v[2 * i + 1]), __builtin_bit_cast(uint32_t, v[2 * i]), 0x07060302u);
+    return __builtin_bit_cast(bf16x8, u32x4{o[0], o[1], o[2], o[3]});
+}
+
+// code - zero in bytes, columns in the order 0 4 1 5, 2 6 3 7: no borrow leaves a byte that has 128 added.
 __device__ inline u32x2 weights_i8(uint32_t w, uint32_t zero4)
 {
     u32x2 v;
-    v[0] = (((w & 0x0f0f0f0fu) | 0x80808080u) - zero4) ^ 0x80808080u;
-    v[1] = ((((w >> 4) & 0x0f0f0f0fu) | 0x80808080u) - zero4) ^ 0x80808080u;
+    v[0] = (((w & 0x0f0f0f0fu) ^ 0x88888888u) - zero4) ^ 0x80808080u;
+    v[1] = ((((w >> 4) & 0x0f0f0f0fu) ^ 0x88888888u) - zero4) ^ 0x80808080u;
     return v;
 }
 
+// What a whole number of the products' second operand stands for.
+template <int BT> constexpr float WEIGHT_UNIT = BT == SPMM_F32 || BT == SPMM_BF16 ? 16.0f : 1.0f;
+
 // ---- the product ---------------------------------------------------------------------------------------------
 
-template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N, tensor C)
+template <int BT, int NT, bool ZEROS> __global__ __launch_bounds__(64 * WAVES) void product_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N, tensor C)
 {
     __shared__ float sums[WAVES][NT][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
@@ -230,7 +243,7 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
     for (int t = 0; t < NT; ++t) tiles[t] = B + min(tile0 + t, token_tiles - 1) * W.blocks * BLOCK_BYTES + lane * 16;
     const uint32_t *codes = W.codes + row_tile * W.blocks * BLOCK_WORDS + lane * 4;
     const float *scales = W.scales + row_tile * W.groups * TILE_ROWS + r;
-    const uint8_t *zeros = W.zeros ? W.zeros + row_tile * W.groups * TILE_ROWS + r : nullptr;
+    const uint8_t *zeros = ZEROS ? W.zeros + row_tile * W.groups * TILE_ROWS + r : nullptr;
 
     f32x4 acc[NT];
 #pragma unroll
@@ -243,7 +256,7 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
         if constexpr (BT == SPMM_I8) {
             i32x4 part[NT];
             auto flush = [&](int s) {
-                const float scale = scales[group_of(s) * TILE_ROWS];
+                const float scale = scales[group_of(s) * TILE_ROWS] * WEIGHT_UNIT<BT>;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -254,8 +267,8 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
                 i32x4 a[NT];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) a[t] = *reinterpret_cast<const i32x4 *>(tiles[t] + at + (s / 2) * 1024);
-                const uint32_t zero0 = (zeros ? zeros[group_of(s) * TILE_ROWS] : 8) * 0x01010101u;
-                const uint32_t zero1 = (zeros ? zeros[group_of(s + 1) * TILE_ROWS] : 8) * 0x01010101u;
+                const uint32_t zero0 = (ZEROS ? zeros[group_of(s) * TILE_ROWS] : 8) * 0x01010101u;
+                const uint32_t zero1 = (ZEROS ? zeros[group_of(s + 1) * TILE_ROWS] : 8) * 0x01010101u;
                 const u32x2 w0 = weights_i8(word[s], zero0), w1 = weights_i8(word[s + 1], zero1);
                 if (per_group == 1) {
 #pragma unroll
@@ -279,7 +292,7 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int group = group_of(s);
-                const int zero = zeros ? zeros[group * TILE_ROWS] : 8;
+                const int zero = ZEROS ? zeros[group * TILE_ROWS] : 8;
                 const bool begins = s % per_group == 0;
                 if (begins)
 #pragma unroll
@@ -289,7 +302,7 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
 #pragma unroll
                     for (int t = 0; t < NT; ++t) part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(tiles[t] + at + s * 1024), w, part[t], 0, 0, 0);
                 } else {
-                    const bf16x8 w = weights_bf16(word[s], zero);
+                    const bf16x8 w = weights_bf16<ZEROS>(word[s], zero);
 #pragma unroll
                     for (int p = PARTS<BT> - 1; p >= 0; --p)
 #pragma unroll
@@ -297,7 +310,7 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
                             part[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8 *>(tiles[t] + at + (s * PARTS<BT> + p) * 1024), w, part[t], 0, 0, 0);
                 }
                 if (s % per_group == per_group - 1) {
-                    const float scale = scales[group * TILE_ROWS];
+                    const float scale = scales[group * TILE_ROWS] * WEIGHT_UNIT<BT>;
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -335,7 +348,7 @@ template <int BT, int NT> __global__ __launch_bounds__(64 * WAVES) void product_
 //              takes six
 //   KWAVES     waves of a workgroup, which share K
 
-template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, bool FMA> __global__ __launch_bounds__(64 * KWAVES) void few_kernel(quant_matrix W, tensor B, const float *B_scales, int32_t N, tensor C)
+template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, bool FMA, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void few_kernel(quant_matrix W, tensor B, const float *B_scales, int32_t N, tensor C)
 {
     __shared__ float sums[KWAVES][RT][256];
     constexpr int SUMS = 4 / PER_GROUP;
@@ -347,7 +360,7 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
     const int64_t tile0 = (int64_t)blockIdx.x * RT;
     const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
     const float *const scales = W.scales + tile0 * W.groups * TILE_ROWS;
-    const uint8_t *const zeros = W.zeros ? W.zeros + tile0 * W.groups * TILE_ROWS : nullptr;
+    const uint8_t *const zeros = ZEROS ? W.zeros + tile0 * W.groups * TILE_ROWS : nullptr;
     const int64_t column = (BY_TOKEN ? 1 : B.ld) * SIZE;  // bytes from one to the next
     const char *const token = B.data + (FMA ? 0 : min(r, N - 1)) * (BY_TOKEN ? B.ld : 1) * SIZE, *const mine = token + 8 * q * column;
     struct asked {
@@ -369,7 +382,7 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
             for (int g = 0; g < SUMS; ++g) {
                 const int64_t group = (int64_t)i * W.groups + (PER_GROUP < 4 ? min(W.groups - 1, b * SUMS + g) : b / group_blocks);
                 a.scale[i][g] = (scales + group * TILE_ROWS)[r];
-                a.zero[i][g] = zeros ? (zeros + group * TILE_ROWS)[r] : 8;
+                a.zero[i][g] = ZEROS ? (zeros + group * TILE_ROWS)[r] : 8;
             }
         }
     };
@@ -384,15 +397,18 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
         }
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
+            // (one tile's weights at a time: the registers do not hold all of them as operands)
+            if (RT > 1) __builtin_amdgcn_sched_barrier(0);
             if constexpr (FMA) {
                 float part = 0.0f;
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     float w[8];
-                    weights_f32(a.word[i][s], a.zero[i][s / PER_GROUP], w);
+                    __builtin_amdgcn_sched_barrier(0);
+                    weights_f32<ZEROS>(a.word[i][s], a.zero[i][s / PER_GROUP], w);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) part = __builtin_fmaf(w[j], a.b[s].v[j], part);
-                    if (s % PER_GROUP == PER_GROUP - 1) acc[i][0] += a.scale[i][s / PER_GROUP] * part, part = 0.0f;
+                    if (s % PER_GROUP == PER_GROUP - 1) acc[i][0] += a.scale[i][s / PER_GROUP] * WEIGHT_UNIT<BT> * part, part = 0.0f;
                 }
             } else if constexpr (BT == SPMM_I8) {
                 u32x2 w[4];
@@ -422,13 +438,13 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
                     if constexpr (BT == SPMM_F16) {
                         part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, o[s].part[0]), weights_f16(a.word[i][s], a.zero[i][s / PER_GROUP]), part, 0, 0, 0);
                     } else {
-                        const bf16x8 w = weights_bf16(a.word[i][s], a.zero[i][s / PER_GROUP]);
+                        const bf16x8 w = weights_bf16<ZEROS>(a.word[i][s], a.zero[i][s / PER_GROUP]);
 #pragma unroll
                         for (int p = PARTS<BT> - 1; p >= 0; --p) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o[s].part[p]), w, part, 0, 0, 0);
                     }
                     if (s % PER_GROUP == PER_GROUP - 1) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][e] += a.scale[i][s / PER_GROUP] * part[e];
+                        for (int e = 0; e < 4; ++e) acc[i][e] += a.scale[i][s / PER_GROUP] * WEIGHT_UNIT<BT> * part[e];
                     }
                 }
             }
@@ -482,13 +498,15 @@ template <int BT, bool BY_TOKEN, bool FMA> hipError_t execute_few(const quant_ma
 {
     auto shaped = [&](auto per_group, auto rt, auto kwaves, auto ahead) {
         constexpr int PER_GROUP = decltype(per_group)::value, RT = decltype(rt)::value, KWAVES = decltype(kwaves)::value, AHEAD = decltype(ahead)::value;
-        return launch_kernel(few_kernel<BT, BY_TOKEN, PER_GROUP, RT, KWAVES, AHEAD, FMA>, dim3((unsigned)((w.tiles + RT - 1) / RT)), 64 * KWAVES, 0, stream, w, B, B_scales,
-                             (int32_t)N, C);
+        const dim3 blocks((unsigned)((w.tiles + RT - 1) / RT));
+        if (w.zeros) return launch_kernel(few_kernel<BT, BY_TOKEN, PER_GROUP, RT, KWAVES, AHEAD, FMA, true>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, (int32_t)N, C);
+        return launch_kernel(few_kernel<BT, BY_TOKEN, PER_GROUP, RT, KWAVES, AHEAD, FMA, false>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, (int32_t)N, C);
     };
     auto run = [&](auto per_group) {
         // (what the registers hold)
-        constexpr int AHEAD = BT == SPMM_F32 && !FMA ? 1 : 2, LESS = decltype(per_group)::value < 4 ? 1 : AHEAD;
-        if (w.tiles >= 1024) return shaped(per_group, constant<4>(), constant<8>(), constant<LESS>());
+        constexpr int AHEAD = BT == SPMM_F32 && !FMA ? 1 : 2, LESS = decltype(per_group)::value < 4 || FMA ? 1 : AHEAD;
+        constexpr int MOST = decltype(per_group)::value == 1 || (BT == SPMM_F32 && !BY_TOKEN) ? 2 : 4;
+        if (w.tiles >= 1024) return shaped(per_group, constant<MOST>(), constant<8>(), constant<LESS>());
         if (w.tiles >= 512) return shaped(per_group, constant<2>(), constant<8>(), constant<AHEAD>());
         if constexpr (BY_TOKEN && BT != SPMM_F32)
             if (w.blocks > 8) return shaped(per_group, constant<1>(), constant<16>(), constant<LESS>());
@@ -524,7 +542,9 @@ template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, con
         if (e != hipSuccess) return e;
         auto product = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
-            return launch_kernel(product_kernel<BT, NT>, dim3((unsigned)w.tiles, (unsigned)((tiles + NT - 1) / NT)), 64 * WAVES, 0, stream, w, (const char *)workspace, scales, n, c);
+            const dim3 blocks((unsigned)w.tiles, (unsigned)((tiles + NT - 1) / NT));
+            if (w.zeros) return launch_kernel(product_kernel<BT, NT, true>, blocks, 64 * WAVES, 0, stream, w, (const char *)workspace, scales, n, c);
+            return launch_kernel(product_kernel<BT, NT, false>, blocks, 64 * WAVES, 0, stream, w, (const char *)workspace, scales, n, c);
         };
         if (tiles <= 2) e = product(std::integral_constant<int, 2>());
         else if (tiles <= 4) e = product(std::integral_constant<int, 4>());

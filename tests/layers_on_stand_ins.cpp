@@ -88,7 +88,7 @@ static void layout(int64_t M, int64_t K, int64_t group, bool zeros)
             const int64_t tile = m / 16, r = m % 16, block = k / 128, s = k % 128 / 32, q = k % 32 / 8, j = k % 8;
             int nibble = 0;
             while (layers::NIBBLE_COLUMN[nibble] != j) ++nibble;
-            const uint32_t code = w.codes[((tile * w.blocks + block) * 64 + q * 16 + r) * 4 + s] >> (4 * nibble) & 15;
+            const uint32_t code = 8 ^ w.codes[((tile * w.blocks + block) * 64 + q * 16 + r) * 4 + s] >> (4 * nibble) & 15u;
             const int64_t g = k / group < groups ? k / group : groups - 1, at = (tile * groups + g) * 16 + r;
             const int zero = zeros ? w.zeros[at] : 8;
             if (m < M && k < K) CHECK((int)code == (codes[(size_t)(m * row + k / 2)] >> (4 * (k & 1)) & 15));
@@ -146,6 +146,8 @@ static void product_refusals()
     CHECK(spmm_quant_create(&plan, 2, 4, 32, codes, scales, zeros) == SPMM_ERR_INVALID_ARG);
     zeros[1] = 15;
     scales[1] = INFINITY;
+    CHECK(spmm_quant_create(&plan, 2, 4, 32, codes, scales, zeros) == SPMM_ERR_INVALID_ARG);
+    scales[1] = 2e36f;
     CHECK(spmm_quant_create(&plan, 2, 4, 32, codes, scales, zeros) == SPMM_ERR_INVALID_ARG);
     scales[1] = NAN;
     CHECK(spmm_quant_create(&plan, 2, 4, 32, codes, scales, zeros) == SPMM_ERR_INVALID_ARG);
