@@ -228,114 +228,150 @@ __device__ inline u32x2 weights_i8(uint32_t w, uint32_t zero4)
 // What a whole number of the products' second operand stands for.
 template <int BT> constexpr float WEIGHT_UNIT = BT == SPMM_F32 || BT == SPMM_BF16 ? 16.0f : 1.0f;
 
-// ---- the product ---------------------------------------------------------------------------------------------
+// ---- many tokens -----------------------------------------------------------------------------------------------
+//
+// A wave has RT tiles of rows and NT tiles of tokens, a workgroup KWAVES such waves that share K; their sums meet in LDS.  Weights become operands once a block and
+// are used for all of its tokens, B (laid out by pack_kernel) comes a tile of tokens at a time, the next one while one is multiplied.
 
-template <int BT, int NT, bool ZEROS> __global__ __launch_bounds__(64 * WAVES) void product_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N, tensor C)
+template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void many_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N,
+                                                                                                                          tensor C)
 {
-    __shared__ float sums[WAVES][NT][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
-    const int64_t row_tile = blockIdx.x, token_tiles = (N + 15) / 16, tile0 = (int64_t)blockIdx.y * NT;
-    const int per_group = W.group < BLOCK_COLS ? (int)W.group / 32 : 4;   // steps behind which a group's sum is full
-    const int group_blocks = W.group < BLOCK_COLS ? 1 : (int)(W.group / BLOCK_COLS), groups_block = W.group < BLOCK_COLS ? BLOCK_COLS / (int)W.group : 1;
-    constexpr int BLOCK_BYTES = 4 * PARTS<BT> * STEP_BYTES<BT>;
-    const char *tiles[NT];
+    // K goes by pieces of STEPS steps of 32 columns, which lie in one group.
+    extern __shared__ float sums[];  // [KWAVES][RT][NT][256]
+    constexpr int PIECES = 4 / STEPS, P = PARTS<BT>, BLOCK_BYTES = 4 * P * STEP_BYTES<BT>, LOADS = BT == SPMM_I8 ? (STEPS + 1) / 2 : STEPS * P;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
+    const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * NT, tile0 = (int64_t)blockIdx.x * RT;
+    const int group_pieces = (int)(W.group / (32 * STEPS)), pieces = W.blocks * PIECES;
+    const int first = (int)((int64_t)pieces * wave / KWAVES), last = (int)((int64_t)pieces * (wave + 1) / KWAVES);
+    const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
+    const float *const scales = W.scales + tile0 * W.groups * TILE_ROWS;
+    const uint8_t *const zeros = ZEROS ? W.zeros + tile0 * W.groups * TILE_ROWS : nullptr;
+    struct asked {
+        uint32_t word[RT][STEPS];
+        float scale[RT];
+        int zero[RT];
+    };
+    auto ask = [&](int piece, asked &a) {
+        const int group = min(piece / group_pieces, W.groups - 1);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) tiles[t] = B + min(tile0 + t, token_tiles - 1) * W.blocks * BLOCK_BYTES + lane * 16;
-    const uint32_t *codes = W.codes + row_tile * W.blocks * BLOCK_WORDS + lane * 4;
-    const float *scales = W.scales + row_tile * W.groups * TILE_ROWS + r;
-    const uint8_t *zeros = ZEROS ? W.zeros + row_tile * W.groups * TILE_ROWS + r : nullptr;
-
-    f32x4 acc[NT];
+        for (int i = 0; i < RT; ++i) {
+            const uint32_t *at = codes + ((int64_t)i * W.blocks + piece / PIECES) * BLOCK_WORDS + piece % PIECES * STEPS + lane * 4;
+            if constexpr (STEPS == 4) {
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(at);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0, 0, 0, 0};
-    const int first = (int)((int64_t)W.blocks * wave / WAVES), last = (int)((int64_t)W.blocks * (wave + 1) / WAVES);
-    for (int b = first; b < last; ++b) {
-        const u32x4 word = *reinterpret_cast<const u32x4 *>(codes + (int64_t)b * BLOCK_WORDS);
-        const int64_t at = (int64_t)b * BLOCK_BYTES;
-        auto group_of = [&](int s) { return min(W.groups - 1, groups_block > 1 ? b * groups_block + s / per_group : b / group_blocks); };
-        if constexpr (BT == SPMM_I8) {
-            i32x4 part[NT];
-            auto flush = [&](int s) {
-                const float scale = scales[group_of(s) * TILE_ROWS] * WEIGHT_UNIT<BT>;
+                for (int s = 0; s < STEPS; ++s) a.word[i][s] = v[s];
+            } else if constexpr (STEPS == 2) {
+                const u32x2 v = *reinterpret_cast<const u32x2 *>(at);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t][i] += scale * (float)part[t][i];
-            };
-#pragma unroll
-            for (int s = 0; s < 4; s += 2) {
-                i32x4 a[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) a[t] = *reinterpret_cast<const i32x4 *>(tiles[t] + at + (s / 2) * 1024);
-                const uint32_t zero0 = (ZEROS ? zeros[group_of(s) * TILE_ROWS] : 8) * 0x01010101u;
-                const uint32_t zero1 = (ZEROS ? zeros[group_of(s + 1) * TILE_ROWS] : 8) * 0x01010101u;
-                const u32x2 w0 = weights_i8(word[s], zero0), w1 = weights_i8(word[s + 1], zero1);
-                if (per_group == 1) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const long w = __builtin_bit_cast(long, h ? w1 : w0);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-                            part[t] = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)(uint32_t)a[t][2 * h] | ((long)a[t][2 * h + 1] << 32), w, i32x4{0, 0, 0, 0}, 0, 0, 0);
-                        flush(s + h);
-                    }
-                } else {
-                    const i32x4 w = {(int)w0[0], (int)w0[1], (int)w1[0], (int)w1[1]};
-                    const bool begins = s == 0 || per_group == 2;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) part[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t], w, begins ? i32x4{0, 0, 0, 0} : part[t], 0, 0, 0);
-                    if (s == 2 || per_group == 2) flush(s);
-                }
+                for (int s = 0; s < STEPS; ++s) a.word[i][s] = v[s];
+            } else {
+                a.word[i][0] = *at;
             }
+            a.scale[i] = (scales + ((int64_t)i * W.groups + group) * TILE_ROWS)[r] * WEIGHT_UNIT<BT>;
+            a.zero[i] = ZEROS ? (zeros + ((int64_t)i * W.groups + group) * TILE_ROWS)[r] : 8;
+        }
+    };
+    // Tiles of tokens past the last: the last one again (not stored).  Codes of one step are half of a lane's 16 bytes.
+    auto ask_tokens = [&](int piece, int t, u32x4(&x)[LOADS]) {
+        const char *at = B + (min(token0 + t, token_tiles - 1) * W.blocks + piece / PIECES) * BLOCK_BYTES;
+        if constexpr (BT == SPMM_I8 && STEPS == 1) {
+            const u32x2 v = *reinterpret_cast<const u32x2 *>(at + piece % PIECES / 2 * 1024 + lane * 16 + piece % 2 * 8);
+            x[0][0] = v[0], x[0][1] = v[1];
         } else {
-            f32x4 part[NT];
+            at += piece % PIECES * (STEPS * P * STEP_BYTES<BT>);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int group = group_of(s);
-                const int zero = ZEROS ? zeros[group * TILE_ROWS] : 8;
-                const bool begins = s % per_group == 0;
-                if (begins)
+            for (int l = 0; l < LOADS; ++l) x[l] = reinterpret_cast<const u32x4 *>(at + l * 1024)[lane];
+        }
+    };
+    f32x4 acc[RT][NT];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) part[t] = f32x4{0, 0, 0, 0};
-                if constexpr (BT == SPMM_F16) {
-                    const f16x8 w = weights_f16(word[s], zero);
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(tiles[t] + at + s * 1024), w, part[t], 0, 0, 0);
+        for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
+    asked now, next;
+    u32x4 x[2][LOADS];
+    if (first < last) ask(first, now), ask_tokens(first, 0, x[0]);
+    for (int piece = first; piece < last; ++piece) {
+        if (piece + 1 < last) ask(piece + 1, next);
+        // W as operands: four words of a step, of two steps for codes
+        u32x4 w[RT][STEPS];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                if constexpr (BT == SPMM_I8) {
+                    const u32x2 v = weights_i8(now.word[i][s], (uint32_t)now.zero[i] * 0x01010101u);
+                    w[i][s / 2][2 * (s % 2)] = v[0], w[i][s / 2][2 * (s % 2) + 1] = v[1];
+                } else if constexpr (BT == SPMM_F16) {
+                    w[i][s] = __builtin_bit_cast(u32x4, weights_f16(now.word[i][s], now.zero[i]));
                 } else {
-                    const bf16x8 w = weights_bf16<ZEROS>(word[s], zero);
-#pragma unroll
-                    for (int p = PARTS<BT> - 1; p >= 0; --p)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-                            part[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8 *>(tiles[t] + at + (s * PARTS<BT> + p) * 1024), w, part[t], 0, 0, 0);
-                }
-                if (s % per_group == per_group - 1) {
-                    const float scale = scales[group * TILE_ROWS] * WEIGHT_UNIT<BT>;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[t][i] += scale * part[t][i];
+                    w[i][s] = __builtin_bit_cast(u32x4, weights_bf16<ZEROS>(now.word[i][s], now.zero[i]));
                 }
             }
         }
-    }
-
-    // The waves' sums meet in LDS, in wave order.
 #pragma unroll
-    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(&sums[wave][t][lane * 4]) = acc[t];
+        for (int t = 0; t < NT; ++t) {
+            u32x4(&a)[LOADS] = x[t & 1];
+            if (t + 1 < NT) ask_tokens(piece, t + 1, x[(t + 1) & 1]);
+            else if (piece + 1 < last) ask_tokens(piece + 1, 0, x[(t + 1) & 1]);
+            if constexpr (BT == SPMM_I8) {
+                i32x4 part[RT];
+                if constexpr (STEPS == 1) {
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+                        part[i] = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)((uint64_t)a[0][0] | (uint64_t)a[0][1] << 32), (long)((uint64_t)w[i][0][0] | (uint64_t)w[i][0][1] << 32),
+                                                                        i32x4{0, 0, 0, 0}, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < STEPS / 2; ++s)
+#pragma unroll
+                        for (int i = 0; i < RT; ++i)
+                            part[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a[s]), __builtin_bit_cast(i32x4, w[i][s]), s == 0 ? i32x4{0, 0, 0, 0} : part[i], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][t][e] += now.scale[i] * (float)part[i][e];
+            } else {
+                f32x4 part[RT];
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) {
+                            const f32x4 from = s == 0 && p == P - 1 ? f32x4{0, 0, 0, 0} : part[i];
+                            if constexpr (BT == SPMM_F16) part[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a[s]), __builtin_bit_cast(f16x8, w[i][s]), from, 0, 0, 0);
+                            else part[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[s * P + p]), __builtin_bit_cast(bf16x8, w[i][s]), from, 0, 0, 0);
+                        }
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][t][e] += now.scale[i] * part[i][e];
+            }
+        }
+        now = next;
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(sums + ((wave * RT + i) * NT + t) * 256 + lane * 4) = acc[i][t];
     __syncthreads();
-    for (int e = threadIdx.x; e < NT * 256; e += 64 * WAVES) {
-        const int m = C.by_token ? e % 16 : e / (16 * NT), t = C.by_token ? e / 16 : e % (16 * NT);
-        const int64_t row = row_tile * TILE_ROWS + m, n = tile0 * 16 + t;
+    // the waves' sums, in wave order: a thread an element of C
+    for (int e = threadIdx.x; e < RT * NT * 256; e += 64 * KWAVES) {
+        const int m = C.by_token ? e % (16 * RT) : e / (16 * NT), t = C.by_token ? e / (16 * RT) : e % (16 * NT);
+        const int64_t row = tile0 * TILE_ROWS + m, n = token0 * 16 + t;
         if (row >= W.M || n >= N) continue;
-        const int at = ((t & 15) >> 2) * 64 + m * 4 + (t & 3);
+        const int at = ((m / 16) * NT + t / 16) * 256 + ((t & 15) >> 2) * 64 + (m % 16) * 4 + (t & 3);
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += sums[w][t >> 4][at];
+        for (int w = 0; w < KWAVES; ++w) v += sums[w * RT * NT * 256 + at];
         if (BT == SPMM_I8) v *= B_scales[n];
         store_as(C.data, C.by_token ? n * C.ld + row : row * C.ld + n, C.type, v);
     }
 }
+
+template <int V> using constant = std::integral_constant<int, V>;
 
 // ---- few tokens ------------------------------------------------------------------------------------------------
 //
@@ -492,8 +528,6 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
     }
 }
 
-template <int V> using constant = std::integral_constant<int, V>;
-
 template <int BT, bool BY_TOKEN, bool FMA> hipError_t execute_few(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
     auto shaped = [&](auto per_group, auto rt, auto kwaves, auto ahead) {
@@ -515,6 +549,30 @@ template <int BT, bool BY_TOKEN, bool FMA> hipError_t execute_few(const quant_ma
     if (w.group == 32) return run(constant<1>());
     if (w.group == 64) return run(constant<2>());
     return run(constant<4>());
+}
+
+template <int BT, int NT, int RT, int KWAVES> hipError_t launch_many(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
+{
+    const dim3 blocks((unsigned)((w.tiles + RT - 1) / RT), (unsigned)((N + 16 * NT - 1) / (16 * NT)));
+    auto shaped = [&](auto per_group, auto zeros) {
+        constexpr int PER_GROUP = decltype(per_group)::value;
+        constexpr bool ZEROS = decltype(zeros)::value;
+        constexpr unsigned LDS = KWAVES * RT * NT * 1024;
+        return launch_kernel(many_kernel<BT, NT, RT, KWAVES, PER_GROUP, ZEROS>, blocks, 64 * KWAVES, LDS, stream, w, B, B_scales, N, C);
+    };
+    auto run = [&](auto per_group) { return w.zeros ? shaped(per_group, std::true_type()) : shaped(per_group, std::false_type()); };
+    if (w.group == 32) return run(constant<1>());
+    if (w.group == 64) return run(constant<2>());
+    return run(constant<4>());
+}
+
+template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
+{
+    if (N <= 32) return launch_many<BT, 2, 1, 8>(w, B, B_scales, N, C, stream);
+    if (N <= 64) return launch_many<BT, 4, 1, 8>(w, B, B_scales, N, C, stream);
+    const int64_t columns = (N + 127) / 128;
+    if ((w.tiles + 3) / 4 * columns >= 192) return launch_many<BT, 8, 4, 4>(w, B, B_scales, N, C, stream);
+    return launch_many<BT, 8, 1, 8>(w, B, B_scales, N, C, stream);
 }
 
 template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, char *workspace, hipStream_t stream)
@@ -540,15 +598,7 @@ template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, con
         if (w.blocks > 0 && b.by_token) e = launch_kernel(pack_kernel<BT, true>, grid, 256, 0, stream, b, w.K, n, w.blocks, workspace);
         else if (w.blocks > 0) e = launch_kernel(pack_kernel<BT, false>, grid, 256, 0, stream, b, w.K, n, w.blocks, workspace);
         if (e != hipSuccess) return e;
-        auto product = [&](auto nt) {
-            constexpr int NT = decltype(nt)::value;
-            const dim3 blocks((unsigned)w.tiles, (unsigned)((tiles + NT - 1) / NT));
-            if (w.zeros) return launch_kernel(product_kernel<BT, NT, true>, blocks, 64 * WAVES, 0, stream, w, (const char *)workspace, scales, n, c);
-            return launch_kernel(product_kernel<BT, NT, false>, blocks, 64 * WAVES, 0, stream, w, (const char *)workspace, scales, n, c);
-        };
-        if (tiles <= 2) e = product(std::integral_constant<int, 2>());
-        else if (tiles <= 4) e = product(std::integral_constant<int, 4>());
-        else e = product(std::integral_constant<int, 8>());
+        e = execute_many<BT>(w, workspace, scales, n, c, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
