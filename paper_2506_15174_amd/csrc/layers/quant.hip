@@ -289,8 +289,14 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
     asked now, next;
-    u32x4 x[2][LOADS];
-    if (first < last) ask(first, now), ask_tokens(first, 0, x[0]);
+    // B of AHEAD tiles of tokens is on its way while one is multiplied: what the registers hold
+    constexpr int ROOM = BT == SPMM_F32 ? 2 : BT == SPMM_I8 ? 8 : 4, AHEAD = ROOM < NT ? ROOM : NT;
+    u32x4 x[AHEAD][LOADS];
+    if (first < last) {
+        ask(first, now);
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t) ask_tokens(first, t, x[t]);
+    }
     for (int piece = first; piece < last; ++piece) {
         if (piece + 1 < last) ask(piece + 1, next);
         // W as operands: four words of a step, of two steps for codes
@@ -311,9 +317,7 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            u32x4(&a)[LOADS] = x[t & 1];
-            if (t + 1 < NT) ask_tokens(piece, t + 1, x[(t + 1) & 1]);
-            else if (piece + 1 < last) ask_tokens(piece + 1, 0, x[(t + 1) & 1]);
+            u32x4(&a)[LOADS] = x[t % AHEAD];
             if constexpr (BT == SPMM_I8) {
                 i32x4 part[RT];
                 if constexpr (STEPS == 1) {
@@ -349,6 +353,8 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][t][e] += now.scale[i] * part[i][e];
             }
+            if (t + AHEAD < NT) ask_tokens(piece, t + AHEAD, x[t % AHEAD]);
+            else if (piece + 1 < last) ask_tokens(piece + 1, t + AHEAD - NT, x[t % AHEAD]);
         }
         now = next;
     }
