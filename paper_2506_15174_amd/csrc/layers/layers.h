@@ -17,8 +17,9 @@ namespace layers {
 // one of 64 two by two, in one of 32 each.  Inside a word nibble i holds j = NIBBLE_COLUMN[i]: a shift by 4 i and one mask give
 // the neighbours 2 i and 2 i + 1 in the low halves of a 32-bit word, as 16-bit operands are held.  A nibble is code - 8 in two's complement.
 //
-// Scales and zero points are [tile][group][TILE_ROWS].  Rows past M have scale 0, columns past K the code of their
-// group's zero point, so that they are whole numbers of 0.  Memory is there for whole TILES_OF tiles, rows past M as above: a wave may have
+// Scales and zero points are [tile][span][TILE_ROWS][groups of a span]: a span is a group, or the groups of a block where they are
+// shorter, which a lane reads at once.  Rows past M and groups past K have scale 0 and zero point 8, columns past K the code of
+// their group's zero point, so that they are whole numbers of 0.  Memory is there for whole TILES_OF tiles, rows past M as above: a wave may have
 // that many.
 constexpr int TILE_ROWS = 16, BLOCK_COLS = 128, BLOCK_WORDS = TILE_ROWS * BLOCK_COLS / 8, TILES_OF = 4;
 constexpr int NIBBLE_COLUMN[8] = {0, 2, 4, 6, 1, 3, 5, 7};
@@ -26,6 +27,7 @@ constexpr int NIBBLE_COLUMN[8] = {0, 2, 4, 6, 1, 3, 5, 7};
 struct quant_matrix {
     int64_t M, K, group;
     int32_t tiles, blocks, groups;  // ceil(M / 16), ceil(K / 128), ceil(K / group)
+    int32_t spans, span_groups;     // spans of K, groups of one
     const uint32_t *codes;          // DEVICE
     const float *scales;
     const uint8_t *zeros;           // NULL: 8 everywhere

@@ -108,10 +108,11 @@ void lay_out(const quant_matrix &w, int64_t t0, int64_t t1, const uint8_t *codes
         for (int r = 0; r < TILE_ROWS; ++r) {
             const int64_t m = tile * TILE_ROWS + r;
             const bool there = m < w.M;
-            for (int64_t g = 0; g < w.groups; ++g) {
-                const int64_t at = (tile * w.groups + g) * TILE_ROWS + r;
-                out_scales[at] = there ? scales[m * w.groups + g] : 0.0f;
-                if (out_zeros) out_zeros[at] = there ? zeros[m * w.groups + g] : 8;
+            for (int64_t g = 0; g < (int64_t)w.spans * w.span_groups; ++g) {
+                const int64_t at = ((tile * w.spans + g / w.span_groups) * TILE_ROWS + r) * w.span_groups + g % w.span_groups;
+                const bool group_there = there && g < w.groups;
+                out_scales[at] = group_there ? scales[m * w.groups + g] : 0.0f;
+                if (out_zeros) out_zeros[at] = group_there ? zeros[m * w.groups + g] : 8;
             }
             for (int64_t b = 0; b < w.blocks; ++b) {
                 uint32_t *block = out_codes + (tile * w.blocks + b) * BLOCK_WORDS + r * 4;
@@ -122,7 +123,7 @@ void lay_out(const quant_matrix &w, int64_t t0, int64_t t1, const uint8_t *codes
                         if (there && k + 8 <= w.K) {
                             std::memcpy(&v, codes + m * row_bytes + k / 2, 4);
                         } else {
-                            const uint32_t zero = there && zeros && w.groups > 0 ? zeros[m * w.groups + std::min<int64_t>(w.groups - 1, k / w.group)] : 8u;
+                            const uint32_t zero = there && zeros && k / w.group < w.groups ? zeros[m * w.groups + k / w.group] : 8u;
                             for (int j = 0; j < 8; ++j) {
                                 const uint32_t c = there && k + j < w.K ? (codes[m * row_bytes + (k + j) / 2] >> (4 * (j & 1))) & 15u : zero;
                                 v |= c << (4 * j);
@@ -144,6 +145,7 @@ spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, c
     quant_matrix &w = p->w;
     w.M = M, w.K = K, w.group = group;
     w.tiles = (int32_t)parts_of(M, TILE_ROWS), w.blocks = (int32_t)parts_of(K, BLOCK_COLS), w.groups = (int32_t)parts_of(K, group);
+    w.span_groups = group < BLOCK_COLS ? (int32_t)(BLOCK_COLS / group) : 1, w.spans = group < BLOCK_COLS ? w.blocks : w.groups;
     const int64_t n_scales = M * w.groups;
     if (M > 0 && K > 0) {
         if (!codes || !scales) return SPMM_ERR_INVALID_ARG;
@@ -152,7 +154,7 @@ spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, c
     }
     hipError_t e = hipGetDevice(&p->device);
     if (e != hipSuccess) return status_of(e);
-    const int64_t tiles = up_to(w.tiles, TILES_OF), code_bytes = tiles * w.blocks * BLOCK_WORDS * 4, padded = tiles * w.groups * TILE_ROWS;
+    const int64_t tiles = up_to(w.tiles, TILES_OF), code_bytes = tiles * w.blocks * BLOCK_WORDS * 4, padded = tiles * w.spans * w.span_groups * TILE_ROWS;
     const int64_t scales_at = up_to(code_bytes, 256), zeros_at = scales_at + up_to(padded * 4, 256);
     p->bytes = zeros_at + (zeros ? up_to(padded, 256) : 0);
     if (code_bytes > 0) {

@@ -225,6 +225,30 @@ __device__ inline u32x2 weights_i8(uint32_t w, uint32_t zero4)
     return v;
 }
 
+// What a lane's row has in a span of K: a scale and a zero point for each group.
+template <int GROUPS, bool ZEROS> struct span_values {
+    float scale[GROUPS];
+    uint32_t zeros;  // a byte each
+    __device__ int zero(int g) const { return ZEROS ? (int)(zeros >> (8 * g) & 15u) : 8; }
+};
+
+// Of row r of a tile of rows, at the span that holds `block`.
+template <int GROUPS, bool ZEROS> __device__ inline span_values<GROUPS, ZEROS> span_of(const quant_matrix &W, int64_t tile, int block, int r)
+{
+    const int span = GROUPS > 1 || W.group == BLOCK_COLS ? block : block / (int)(W.group / BLOCK_COLS);
+    const int64_t at = (tile * W.spans + span) * (TILE_ROWS * GROUPS);
+    span_values<GROUPS, ZEROS> v;
+    const neighbours<float, GROUPS> s = reinterpret_cast<const neighbours<float, GROUPS> *>(W.scales + at)[r];
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) v.scale[g] = s.v[g];
+    v.zeros = 0;
+    if constexpr (ZEROS) {
+        typedef std::conditional_t<GROUPS == 4, uint32_t, std::conditional_t<GROUPS == 2, uint16_t, uint8_t>> packed;
+        v.zeros = reinterpret_cast<const packed *>(W.zeros + at)[r];
+    }
+    return v;
+}
+
 // What a whole number of the products' second operand stands for.
 template <int BT> constexpr float WEIGHT_UNIT = BT == SPMM_F32 || BT == SPMM_BF16 ? 16.0f : 1.0f;
 
@@ -241,21 +265,19 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
     constexpr int PIECES = 4 / STEPS, P = PARTS<BT>, BLOCK_BYTES = 4 * P * STEP_BYTES<BT>, LOADS = BT == SPMM_I8 ? (STEPS + 1) / 2 : STEPS * P;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
     const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * NT, tile0 = (int64_t)blockIdx.x * RT;
-    const int group_pieces = (int)(W.group / (32 * STEPS)), pieces = W.blocks * PIECES;
+    const int pieces = W.blocks * PIECES;
     const int first = (int)((int64_t)pieces * wave / KWAVES), last = (int)((int64_t)pieces * (wave + 1) / KWAVES);
     const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
-    const float *const scales = W.scales + tile0 * W.groups * TILE_ROWS;
-    const uint8_t *const zeros = ZEROS ? W.zeros + tile0 * W.groups * TILE_ROWS : nullptr;
     struct asked {
         uint32_t word[RT][STEPS];
         float scale[RT];
         int zero[RT];
     };
     auto ask = [&](int piece, asked &a) {
-        const int group = min(piece / group_pieces, W.groups - 1);
+        const int block = piece / PIECES, of_block = piece % PIECES, span = PIECES > 1 || W.group == BLOCK_COLS ? block : block / (int)(W.group / BLOCK_COLS);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const uint32_t *at = codes + ((int64_t)i * W.blocks + piece / PIECES) * BLOCK_WORDS + piece % PIECES * STEPS + lane * 4;
+            const uint32_t *at = codes + ((int64_t)i * W.blocks + block) * BLOCK_WORDS + of_block * STEPS + lane * 4;
             if constexpr (STEPS == 4) {
                 const u32x4 v = *reinterpret_cast<const u32x4 *>(at);
 #pragma unroll
@@ -267,8 +289,9 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
             } else {
                 a.word[i][0] = *at;
             }
-            a.scale[i] = (scales + ((int64_t)i * W.groups + group) * TILE_ROWS)[r] * WEIGHT_UNIT<BT>;
-            a.zero[i] = ZEROS ? (zeros + ((int64_t)i * W.groups + group) * TILE_ROWS)[r] : 8;
+            const int64_t values = ((tile0 + i) * W.spans + span) * (TILE_ROWS * PIECES) + of_block;
+            a.scale[i] = (W.scales + values)[r * PIECES] * WEIGHT_UNIT<BT>;
+            a.zero[i] = ZEROS ? (W.zeros + values)[r * PIECES] : 8;
         }
     };
     // Tiles of tokens past the last: the last one again (not stored).  Codes of one step are half of a lane's 16 bytes.
@@ -377,6 +400,159 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
     }
 }
 
+// ---- prompts -----------------------------------------------------------------------------------------------------
+//
+// A wave has 64 rows and 64 tokens (32 in fp32, whose three parts take the registers).  Of a workgroup's eight, ROW_WAVES lie one below the other and share their tokens' B, TOKEN_WAVES side by side, and K_WAVES
+// such groups share K; their sums meet in LDS at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock (1 KiB feeds four
+// instructions of 16 clocks on each of four SIMDs); it is on its way there by stages of STAGE steps of 32 columns while the stage before is multiplied.  Weights are made operands by
+// each wave for itself: 52 instructions a step beside 16 of the matrix unit, two waves to a SIMD, is about what keeps both busy.
+
+template <int BT> constexpr int WIDE_NT = BT == SPMM_F32 ? 2 : 4;
+
+template <int BT, int ROW_WAVES, int TOKEN_WAVES, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N, tensor C)
+{
+    extern __shared__ __align__(16) char lds[];
+    constexpr int RT = 4, NT = WIDE_NT<BT>, K_WAVES = 8 / (ROW_WAVES * TOKEN_WAVES), TILES = NT * TOKEN_WAVES, SUMS = 4 / STEPS, P = PARTS<BT>, BLOCK_BYTES = 4 * P * STEP_BYTES<BT>;
+    constexpr int STAGE = BT == SPMM_F32 ? 1 : 4, STAGES = 4 / STAGE, TILE_BYTES = BLOCK_BYTES / STAGES, STAGE_BYTES = TILES * TILE_BYTES;
+    constexpr int LOADS = TILE_BYTES / 1024, EACH = TILES * LOADS / ROW_WAVES / TOKEN_WAVES;
+    static_assert(EACH * ROW_WAVES * TOKEN_WAVES == TILES * LOADS);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
+    const int row_wave = wave % ROW_WAVES, token_wave = wave / ROW_WAVES % TOKEN_WAVES, k_wave = wave / (ROW_WAVES * TOKEN_WAVES), sharer = wave % (ROW_WAVES * TOKEN_WAVES);
+    const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * TILES, wg_tile0 = (int64_t)blockIdx.x * (RT * ROW_WAVES);
+    // (a wave whose rows do not exist has the last ones)
+    const int64_t tile0 = min(wg_tile0 + row_wave * RT, ((int64_t)W.tiles - 1) / RT * RT);
+    const int first = (int)((int64_t)W.blocks * k_wave / K_WAVES), last = (int)((int64_t)W.blocks * (k_wave + 1) / K_WAVES);
+    const int rounds = (W.blocks + K_WAVES - 1) / K_WAVES;  // as many for every wave, for the barriers
+    const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
+    struct asked {
+        u32x4 word[RT];
+        span_values<SUMS, ZEROS> span[RT];
+    };
+    auto ask = [&](int b, asked &a) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            a.word[i] = reinterpret_cast<const u32x4 *>(codes + ((int64_t)i * W.blocks + b) * BLOCK_WORDS)[lane];
+            a.span[i] = span_of<SUMS, ZEROS>(W, tile0 + i, b, r);
+        }
+    };
+    // This wave's share of a stage of B, straight to LDS: [place][k_wave][tile of tokens][1 KiB each]
+    auto place_of = [&](int place) { return lds + (place * K_WAVES + k_wave) * STAGE_BYTES; };
+    auto send = [&](int b, int stage, int place) {
+#pragma unroll
+        for (int l = 0; l < EACH; ++l) {
+            const int at = sharer * EACH + l;
+            const char *from = B + (min(token0 + at / LOADS, token_tiles - 1) * W.blocks + b) * BLOCK_BYTES + stage * TILE_BYTES + at % LOADS * 1024 + lane * 16;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)(place_of(place) + at * 1024), 16, 0, 0);
+        }
+    };
+    typedef std::conditional_t<BT == SPMM_I8, i32x4, f32x4> sum;
+    f32x4 acc[RT][NT];
+    sum part[RT][NT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
+    asked now, next;
+    if (first < last) {
+        send(first, 0, 0);
+        ask(first, now);
+    }
+    for (int round = 0; round < rounds; ++round) {
+        const int b = first + round;
+#pragma unroll
+        for (int stage = 0; stage < STAGES; ++stage) {
+            const int place = STAGES > 1 ? stage & 1 : round & 1;
+            // This wave's share of the stage is there (and what it asked for besides), then the others'; all have read the stage before.
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (b >= last) continue;
+            if (stage + 1 < STAGES) send(b, stage + 1, place ^ 1);
+            else if (b + 1 < last) send(b + 1, 0, place ^ 1);
+            if (stage == STAGES - 1 && b + 1 < last) ask(b + 1, next);
+            const char *const from = place_of(place) + token_wave * (NT * TILE_BYTES) + lane * 16;
+#pragma unroll
+            for (int h = 0; h < STAGE; h += BT == SPMM_I8 && STEPS > 1 ? 2 : 1) {
+                const int s = stage * STAGE + h;
+                const bool begins = s % STEPS == 0;
+                if (STEPS < 4) __builtin_amdgcn_sched_barrier(0);  // (scales of several groups: no registers for two steps at a time)
+                if constexpr (BT == SPMM_I8) {
+                    i32x4 x[NT];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const i32x4 *>(from + t * TILE_BYTES + h / 2 * 1024);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        const u32x2 w0 = weights_i8(now.word[i][s], (uint32_t)now.span[i].zero(s / STEPS) * 0x01010101u);
+                        if constexpr (STEPS == 1) {
+#pragma unroll
+                            for (int t = 0; t < NT; ++t)
+                                part[i][t] = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)((uint64_t)(uint32_t)x[t][2 * (h % 2)] | (uint64_t)(uint32_t)x[t][2 * (h % 2) + 1] << 32),
+                                                                                   __builtin_bit_cast(long, w0), sum{0, 0, 0, 0}, 0, 0, 0);
+                        } else {
+                            const u32x2 w1 = weights_i8(now.word[i][s + 1], (uint32_t)now.span[i].zero(s / STEPS) * 0x01010101u);
+                            const i32x4 w = {(int)w0[0], (int)w0[1], (int)w1[0], (int)w1[1]};
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) part[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w, begins ? sum{0, 0, 0, 0} : part[i][t], 0, 0, 0);
+                        }
+                    }
+                } else {
+                    u32x4 w[RT];
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        if constexpr (BT == SPMM_F16) w[i] = __builtin_bit_cast(u32x4, weights_f16(now.word[i][s], now.span[i].zero(s / STEPS)));
+                        else w[i] = __builtin_bit_cast(u32x4, weights_bf16<ZEROS>(now.word[i][s], now.span[i].zero(s / STEPS)));
+                    }
+#pragma unroll
+                    for (int p = P - 1; p >= 0; --p) {
+                        u32x4 x[NT];
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const u32x4 *>(from + t * TILE_BYTES + (h * P + p) * 1024);
+#pragma unroll
+                        for (int i = 0; i < RT; ++i)
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                sum &to = part[i][t];
+                                const sum c = begins && p == P - 1 ? sum{0, 0, 0, 0} : to;
+                                if constexpr (BT == SPMM_F16) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[t]), __builtin_bit_cast(f16x8, w[i]), c, 0, 0, 0);
+                                else to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, w[i]), c, 0, 0, 0);
+                            }
+                    }
+                }
+                if (s % STEPS == STEPS - 1 || (BT == SPMM_I8 && (s + 1) % STEPS == STEPS - 1)) {
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][t][e] += now.span[i].scale[s / STEPS] * WEIGHT_UNIT<BT> * (float)part[i][t][e];
+                }
+            }
+        }
+        now = next;
+    }
+    // The sums of the groups that share K meet in LDS: [k_wave][tile of rows][tile of tokens][256]
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(lds);
+    constexpr int ROW_TILES = RT * ROW_WAVES;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            *reinterpret_cast<f32x4 *>(sums + ((k_wave * ROW_TILES + row_wave * RT + i) * TILES + token_wave * NT + t) * 256 + lane * 4) = acc[i][t];
+    __syncthreads();
+    for (int e = threadIdx.x; e < ROW_TILES * TILES * 256; e += 512) {
+        const int m = C.by_token ? e % (16 * ROW_TILES) : e / (16 * TILES), t = C.by_token ? e / (16 * ROW_TILES) : e % (16 * TILES);
+        const int64_t row = wg_tile0 * TILE_ROWS + m, n = token0 * 16 + t;
+        if (row >= W.M || n >= N) continue;
+        const int at = ((m / 16) * TILES + t / 16) * 256 + ((t & 15) >> 2) * 64 + (m % 16) * 4 + (t & 3);
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K_WAVES; ++k) v += sums[k * ROW_TILES * TILES * 256 + at];
+        if (BT == SPMM_I8) v *= B_scales[n];
+        store_as(C.data, C.by_token ? n * C.ld + row : row * C.ld + n, C.type, v);
+    }
+}
+
 template <int V> using constant = std::integral_constant<int, V>;
 
 // ---- few tokens ------------------------------------------------------------------------------------------------
@@ -396,19 +572,15 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
     constexpr int SUMS = 4 / PER_GROUP;
     constexpr int64_t SIZE = sizeof(typename stored<BT>::type);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
-    const int group_blocks = PER_GROUP < 4 ? 1 : (int)(W.group / BLOCK_COLS);
     const int first = (int)((int64_t)W.blocks * wave / KWAVES), last = (int)((int64_t)W.blocks * (wave + 1) / KWAVES);
     // (the plan's memory has whole fours of row tiles)
     const int64_t tile0 = (int64_t)blockIdx.x * RT;
     const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
-    const float *const scales = W.scales + tile0 * W.groups * TILE_ROWS;
-    const uint8_t *const zeros = ZEROS ? W.zeros + tile0 * W.groups * TILE_ROWS : nullptr;
     const int64_t column = (BY_TOKEN ? 1 : B.ld) * SIZE;  // bytes from one to the next
     const char *const token = B.data + (FMA ? 0 : min(r, N - 1)) * (BY_TOKEN ? B.ld : 1) * SIZE, *const mine = token + 8 * q * column;
     struct asked {
         u32x4 word[RT];
-        float scale[RT][SUMS];
-        int zero[RT][SUMS];
+        span_values<SUMS, ZEROS> span[RT];
         raw<BT> b[4];
     };
     auto ask = [&](int b, asked &a, auto tail) {
@@ -419,14 +591,7 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
 #pragma unroll
         for (int s = 0; s < 4; ++s) a.b[s] = fetch<BT, BY_TOKEN, TAIL>((TAIL ? token : mine) + b * BLOCK_COLS * column, column, 32 * s + (TAIL ? 8 * q : 0), left);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-#pragma unroll
-            for (int g = 0; g < SUMS; ++g) {
-                const int64_t group = (int64_t)i * W.groups + (PER_GROUP < 4 ? min(W.groups - 1, b * SUMS + g) : b / group_blocks);
-                a.scale[i][g] = (scales + group * TILE_ROWS)[r];
-                a.zero[i][g] = ZEROS ? (zeros + group * TILE_ROWS)[r] : 8;
-            }
-        }
+        for (int i = 0; i < RT; ++i) a.span[i] = span_of<SUMS, ZEROS>(W, tile0 + i, b, r);
     };
     f32x4 acc[RT];
 #pragma unroll
@@ -447,15 +612,15 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
                 for (int s = 0; s < 4; ++s) {
                     float w[8];
                     __builtin_amdgcn_sched_barrier(0);
-                    weights_f32<ZEROS>(a.word[i][s], a.zero[i][s / PER_GROUP], w);
+                    weights_f32<ZEROS>(a.word[i][s], a.span[i].zero(s / PER_GROUP), w);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) part = __builtin_fmaf(w[j], a.b[s].v[j], part);
-                    if (s % PER_GROUP == PER_GROUP - 1) acc[i][0] += a.scale[i][s / PER_GROUP] * WEIGHT_UNIT<BT> * part, part = 0.0f;
+                    if (s % PER_GROUP == PER_GROUP - 1) acc[i][0] += a.span[i].scale[s / PER_GROUP] * WEIGHT_UNIT<BT> * part, part = 0.0f;
                 }
             } else if constexpr (BT == SPMM_I8) {
                 u32x2 w[4];
 #pragma unroll
-                for (int s = 0; s < 4; ++s) w[s] = weights_i8(a.word[i][s], a.zero[i][s / PER_GROUP] * 0x01010101u);
+                for (int s = 0; s < 4; ++s) w[s] = weights_i8(a.word[i][s], a.span[i].zero(s / PER_GROUP) * 0x01010101u);
                 i32x4 part;
 #pragma unroll
                 for (int s = 0; s < 4; s += PER_GROUP == 1 ? 1 : 2) {
@@ -469,7 +634,7 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
                     }
                     if (PER_GROUP < 4 || s == 2) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][e] += a.scale[i][s / PER_GROUP] * (float)part[e];
+                        for (int e = 0; e < 4; ++e) acc[i][e] += a.span[i].scale[s / PER_GROUP] * (float)part[e];
                     }
                 }
             } else {
@@ -478,15 +643,15 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
                 for (int s = 0; s < 4; ++s) {
                     if (s % PER_GROUP == 0) part = f32x4{0, 0, 0, 0};
                     if constexpr (BT == SPMM_F16) {
-                        part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, o[s].part[0]), weights_f16(a.word[i][s], a.zero[i][s / PER_GROUP]), part, 0, 0, 0);
+                        part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, o[s].part[0]), weights_f16(a.word[i][s], a.span[i].zero(s / PER_GROUP)), part, 0, 0, 0);
                     } else {
-                        const bf16x8 w = weights_bf16<ZEROS>(a.word[i][s], a.zero[i][s / PER_GROUP]);
+                        const bf16x8 w = weights_bf16<ZEROS>(a.word[i][s], a.span[i].zero(s / PER_GROUP));
 #pragma unroll
                         for (int p = PARTS<BT> - 1; p >= 0; --p) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o[s].part[p]), w, part, 0, 0, 0);
                     }
                     if (s % PER_GROUP == PER_GROUP - 1) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][e] += a.scale[i][s / PER_GROUP] * WEIGHT_UNIT<BT> * part[e];
+                        for (int e = 0; e < 4; ++e) acc[i][e] += a.span[i].scale[s / PER_GROUP] * WEIGHT_UNIT<BT> * part[e];
                     }
                 }
             }
@@ -572,10 +737,28 @@ template <int BT, int NT, int RT, int KWAVES> hipError_t launch_many(const quant
     return run(constant<4>());
 }
 
+template <int BT, int ROW_WAVES, int TOKEN_WAVES> hipError_t launch_wide(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
+{
+    constexpr int ROWS = 4 * ROW_WAVES, TILES = WIDE_NT<BT> * TOKEN_WAVES, K_WAVES = 8 / (ROW_WAVES * TOKEN_WAVES);
+    constexpr unsigned STAGES = 2 * K_WAVES * TILES * PARTS<BT> * STEP_BYTES<BT> * (BT == SPMM_F32 ? 1 : 4), SUMS = 8 * 4 * WIDE_NT<BT> * 1024, LDS = STAGES > SUMS ? STAGES : SUMS;
+    static_assert(LDS <= 160 * 1024);
+    const dim3 blocks((unsigned)((w.tiles + ROWS - 1) / ROWS), (unsigned)((N + 16 * TILES - 1) / (16 * TILES)));
+    auto shaped = [&](auto per_group, auto zeros) {
+        return launch_kernel(wide_kernel<BT, ROW_WAVES, TOKEN_WAVES, decltype(per_group)::value, decltype(zeros)::value>, blocks, 512, LDS, stream, w, B, B_scales, N, C);
+    };
+    auto run = [&](auto per_group) { return w.zeros ? shaped(per_group, std::true_type()) : shaped(per_group, std::false_type()); };
+    if (w.group == 32) return run(constant<1>());
+    if (w.group == 64) return run(constant<2>());
+    return run(constant<4>());
+}
+
 template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
     if (N <= 32) return launch_many<BT, 2, 1, 8>(w, B, B_scales, N, C, stream);
     if (N <= 64) return launch_many<BT, 4, 1, 8>(w, B, B_scales, N, C, stream);
+    // workgroups of 128 rows and 128 tokens (fp32: 64), of which the chip should be full
+    constexpr int64_t WIDE_TOKENS = 32 * WIDE_NT<BT>;
+    if ((w.tiles + 7) / 8 * ((N + WIDE_TOKENS - 1) / WIDE_TOKENS) >= 200) return launch_wide<BT, 2, 2>(w, B, B_scales, N, C, stream);
     const int64_t columns = (N + 127) / 128;
     if ((w.tiles + 3) / 4 * columns >= 192) return launch_many<BT, 8, 4, 4>(w, B, B_scales, N, C, stream);
     return launch_many<BT, 8, 1, 8>(w, B, B_scales, N, C, stream);

@@ -89,12 +89,14 @@ static void layout(int64_t M, int64_t K, int64_t group, bool zeros)
             int nibble = 0;
             while (layers::NIBBLE_COLUMN[nibble] != j) ++nibble;
             const uint32_t code = 8 ^ w.codes[((tile * w.blocks + block) * 64 + q * 16 + r) * 4 + s] >> (4 * nibble) & 15u;
-            const int64_t g = k / group < groups ? k / group : groups - 1, at = (tile * groups + g) * 16 + r;
+            const int64_t span = group < 128 ? 128 / group : 1, spans = group < 128 ? w.blocks : groups, g = k / group;
+            if (g >= spans * span) continue;   // (behind the last span of 256 columns or more)
+            const int64_t at = ((tile * spans + g / span) * 16 + r) * span + g % span;
             const int zero = zeros ? w.zeros[at] : 8;
             if (m < M && k < K) CHECK((int)code == (codes[(size_t)(m * row + k / 2)] >> (4 * (k & 1)) & 15));
             else CHECK((int)code == zero);
-            CHECK(w.scales[at] == (m < M ? scales[(size_t)(m * groups + g)] : 0.0f));
-            if (m < M && zeros) CHECK(zero == z[(size_t)(m * groups + g)]);
+            CHECK(w.scales[at] == (m < M && g < groups ? scales[(size_t)(m * groups + g)] : 0.0f));
+            if (m < M && zeros && g < groups) CHECK(zero == z[(size_t)(m * groups + g)]);
         }
     int64_t info[4];
     CHECK(spmm_quant_describe(plan, info, info + 1, info + 2, info + 3) == SPMM_OK && info[0] == M && info[1] == K && info[2] == group && info[3] > 0);
