@@ -7,6 +7,12 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/Context.h>
+#include <ATen/EmptyTensor.h>
+#include <ATen/hip/impl/HIPCachingAllocatorMasqueradingAsCUDA.h>
+#include <ATen/record_function.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -16,7 +22,6 @@
 #include <stdint.h>
 
 #include <exception>
-#include <optional>
 
 #include "../../../include/spmm_layers.h"
 
@@ -107,12 +112,35 @@ void on_current_device(const at::Tensor &t)
 // By token: a row of memory is a token.
 bool by_token(const at::Tensor &t) { return t.stride(1) != 1 && t.stride(0) == 1; }
 
-at::Tensor made(int64_t rows, int64_t cols, bool tokens_first, at::ScalarType type, const at::Tensor &beside)
-{
-    const at::TensorOptions options = at::TensorOptions().dtype(type).device(beside.device());
-    if (tokens_first) return at::empty({cols, rows}, options).t();
-    return at::empty({rows, cols}, options);
-}
+// Allocations of a call.  On its way through the dispatcher at::empty takes 0.3 us of a small call's 3 to 4, and a norm makes three tensors.  Where nothing may
+// want to see or change those calls (a dispatch mode, a functional transform, inference mode, a profiler, the fill of deterministic mode) they are
+// made from the same allocator directly.
+struct allocations {
+    const at::Tensor &beside;
+    bool plain;
+    explicit allocations(const at::Tensor &t) : beside(t)
+    {
+        const c10::impl::LocalDispatchKeySet local = c10::impl::tls_local_dispatch_key_set();
+        plain = local.included_ == c10::default_included_set && local.excluded_ == c10::default_excluded_set && !c10::impl::TorchDispatchModeTLS::any_modes_set() &&
+                !at::hasCallbacks() && !at::globalContext().deterministicAlgorithms() && t.key_set().has(c10::DispatchKey::CUDA);
+    }
+    at::Tensor strided(at::IntArrayRef sizes, at::IntArrayRef strides, at::ScalarType type) const
+    {
+        if (!plain) return at::empty_strided(sizes, strides, at::TensorOptions().dtype(type).device(beside.device()));
+        return at::Tensor(at::detail::empty_strided_generic(sizes, strides, c10::hip::HIPCachingAllocatorMasqueradingAsCUDA::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type));
+    }
+    // (rows, cols), a row or a column of it in a piece
+    at::Tensor matrix(int64_t rows, int64_t cols, bool columns, at::ScalarType type) const
+    {
+        const int64_t sizes[2] = {rows, cols}, strides[2] = {columns ? 1 : cols, columns ? rows : 1};
+        return strided(sizes, strides, type);
+    }
+    at::Tensor vector(int64_t n, at::ScalarType type) const
+    {
+        const int64_t one = 1;
+        return strided(n, one, type);
+    }
+};
 
 at::ScalarType dtype_of(PyObject *o, at::ScalarType otherwise, unsigned types)
 {
@@ -130,19 +158,48 @@ struct workspace {
     at::Tensor memory;
     void *data = nullptr;
     size_t bytes = 0;
-    void take(size_t n, const at::Tensor &beside)
+    void take(size_t n, const allocations &from)
     {
         if (n == 0) return;
-        memory = at::empty({(int64_t)n}, at::TensorOptions().dtype(at::kByte).device(beside.device()));
+        memory = from.vector((int64_t)n, at::kByte);
         data = memory.data_ptr();
         bytes = n;
     }
 };
 
-PyObject *wrapped(const std::optional<at::Tensor> &t)
+PyObject *wrapped(const at::Tensor &t)
 {
-    if (!t || !t->defined()) Py_RETURN_NONE;
-    return THPVariable_Wrap(*t);
+    if (!t.defined()) Py_RETURN_NONE;
+    return THPVariable_Wrap(t);
+}
+
+// The named tuples of layers.py, which norm and gate answer with.
+PyTypeObject *normed_type = nullptr, *gated_type = nullptr;
+
+PyObject *answer_types(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (nargs != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1]) || !PyType_IsSubtype((PyTypeObject *)args[0], &PyTuple_Type) ||
+        !PyType_IsSubtype((PyTypeObject *)args[1], &PyTuple_Type)) {
+        PyErr_SetString(PyExc_TypeError, "answer_types(Normed, Gated)");
+        return nullptr;
+    }
+    Py_INCREF(args[0]);
+    Py_INCREF(args[1]);
+    normed_type = (PyTypeObject *)args[0], gated_type = (PyTypeObject *)args[1];
+    Py_RETURN_NONE;
+}
+
+// A tuple of the given subclass; takes over the references of `fields`.
+template <int N> PyObject *answer(PyTypeObject *type, PyObject *const (&fields)[N])
+{
+    PyObject *t = type ? type->tp_alloc(type, N) : PyTuple_New(N);
+    for (int i = 0; i < N; ++i) {
+        if (t && fields[i]) PyTuple_SET_ITEM(t, i, fields[i]);
+        else Py_XDECREF(fields[i]);
+    }
+    if (!PyErr_Occurred()) return t;
+    Py_XDECREF(t);
+    return nullptr;
 }
 
 template <typename F> PyObject *guarded(F &&f)
@@ -198,13 +255,14 @@ PyObject *quant_execute(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         spmm_status_t st;
         {
             others_run free_to_run;
-            if (!given) C = made(M, N, by_token(*B), type, *B);
+            const allocations from(*B);
+            if (!given) C = from.matrix(M, N, by_token(*B), type);
             const spmm_tensor_t c = {C.data_ptr(), C.stride(0), C.stride(1), type_of(C.scalar_type())};
             size_t bytes = 0;
             workspace room;
             st = spmm_quant_workspace(plan, b.type, N, &bytes);
             if (st == SPMM_OK) {
-                room.take(bytes, *B);
+                room.take(bytes, from);
                 st = spmm_quant_execute(plan, &b, scales ? static_cast<const float *>(scales->data_ptr()) : nullptr, N, &c, room.data, room.bytes, stream_beside(*B));
             }
         }
@@ -234,10 +292,10 @@ struct outputs {
             scales = *s;
         }
     }
-    void make(const at::Tensor &x, at::ScalarType type)
+    void make(const at::Tensor &x, at::ScalarType type, const allocations &from)
     {
-        if (!out.defined()) out = made(x.size(0), x.size(1), type == at::kChar || by_token(x), type, x);
-        if (type == at::kChar && !scales.defined()) scales = at::empty({x.size(1)}, at::TensorOptions().dtype(at::kFloat).device(x.device()));
+        if (!out.defined()) out = from.matrix(x.size(0), x.size(1), type == at::kChar || by_token(x), type);
+        if (type == at::kChar && !scales.defined()) scales = from.vector(x.size(1), at::kFloat);
     }
 };
 
@@ -283,8 +341,9 @@ PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         spmm_status_t st;
         {
             others_run free_to_run;
-            o.make(*x, type);
-            if (wants && !t) total = made(x->size(0), x->size(1), by_token(*x), x->scalar_type(), *x);
+            const allocations from(*x);
+            o.make(*x, type, from);
+            if (wants && !t) total = from.matrix(x->size(0), x->size(1), by_token(*x), x->scalar_type());
             a.total = as_seen(total);
             a.out = as_seen(o.out);
             a.scales = o.scales.defined() ? static_cast<float *>(o.scales.data_ptr()) : nullptr;
@@ -295,12 +354,12 @@ PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             workspace room;
             st = spmm_norm_workspace(x->size(0), x->size(1), &a, &bytes);
             if (st == SPMM_OK) {
-                room.take(bytes, *x);
+                room.take(bytes, from);
                 st = spmm_norm(x->size(0), x->size(1), &a, room.data, room.bytes, stream_beside(*x));
             }
         }
         if (st != SPMM_OK) return PyLong_FromLong((long)st);
-        return Py_BuildValue("(NNN)", wrapped(o.out), wrapped(total), wrapped(o.scales));
+        return answer<3>(normed_type, {wrapped(o.out), wrapped(total), wrapped(o.scales)});
     });
 }
 
@@ -327,7 +386,8 @@ PyObject *gate(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         spmm_status_t st;
         {
             others_run free_to_run;
-            o.make(*x, type);
+            const allocations from(*x);
+            o.make(*x, type, from);
             g.out = as_seen(o.out);
             g.scales = o.scales.defined() ? static_cast<float *>(o.scales.data_ptr()) : nullptr;
             g.act = (int32_t)act;
@@ -335,12 +395,12 @@ PyObject *gate(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             workspace room;
             st = spmm_gate_workspace(x->size(0), x->size(1), &g, &bytes);
             if (st == SPMM_OK) {
-                room.take(bytes, *x);
+                room.take(bytes, from);
                 st = spmm_gate(x->size(0), x->size(1), &g, room.data, room.bytes, stream_beside(*x));
             }
         }
         if (st != SPMM_OK) return PyLong_FromLong((long)st);
-        return Py_BuildValue("(NN)", wrapped(o.out), wrapped(o.scales));
+        return answer<2>(gated_type, {wrapped(o.out), wrapped(o.scales)});
     });
 }
 
@@ -348,6 +408,7 @@ PyMethodDef methods[] = {
     {"quant_execute", (PyCFunction)(void (*)(void))quant_execute, METH_FASTCALL, "spmm_quant_execute on torch tensors; returns C, or a status code"},
     {"norm", (PyCFunction)(void (*)(void))norm, METH_FASTCALL, "spmm_norm on torch tensors; returns (out, total, scales), or a status code"},
     {"gate", (PyCFunction)(void (*)(void))gate, METH_FASTCALL, "spmm_gate on torch tensors; returns (out, scales), or a status code"},
+    {"answer_types", (PyCFunction)(void (*)(void))answer_types, METH_FASTCALL, "answer_types(Normed, Gated): the tuples that norm and gate answer with"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_spmm_layers", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -7,7 +7,7 @@
 //
 // Codes do not wait for f: they depend on p alone, so one look at the token gives both statistics.  All of it is bound by
 // memory, or by the latency of one launch: elements are read once and held in registers between the statistics
-// and the output (rows_kernel, columns_kernel), up to the lengths that their registers hold.
+// and the output where registers hold them.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -181,53 +181,41 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(1024) vo
 
 // ---- a feature a row of memory ---------------------------------------------------------------------------------
 
-// A workgroup has all features of 16 tokens.  A thread reads 16 bytes of a row, COLS threads lie side by side (64 or 32 bytes of a row), ROWS rows are read
-// at a time; HELD such steps stay in registers (0: any number of them, read twice).
+// Few tokens of not too many features: a workgroup has all features of some tokens.  A thread reads 16 bytes of a row, COLS threads lie side by side, HELD rows stay in
+// a thread's registers.
 template <int TYPE> constexpr int COLUMN_UNIT = TYPE == SPMM_F32 ? 4 : 8;
-constexpr int COLUMN_TOKENS = 16, COLUMN_THREADS = 1024;
-template <int TYPE> constexpr int COLUMN_ROWS = COLUMN_THREADS / (COLUMN_TOKENS / COLUMN_UNIT<TYPE>);
+constexpr int COLUMN_THREADS = 1024;
 
-template <bool NORM, bool CODES, int TYPE, int HELD> __global__ __launch_bounds__(COLUMN_THREADS) void columns_kernel(rows_args a)
+template <bool NORM, bool CODES, int TYPE, int COLS, int HELD> __global__ __launch_bounds__(COLUMN_THREADS) void columns_kernel(rows_args a)
 {
     typedef typename element<TYPE>::type E;
-    constexpr int U = COLUMN_UNIT<TYPE>, COLS = COLUMN_TOKENS / U, ROWS = COLUMN_ROWS<TYPE>, WAVES = COLUMN_THREADS / 64;
-    __shared__ float squares[WAVES][COLUMN_TOKENS], mosts[WAVES][COLUMN_TOKENS], factors[2][COLUMN_TOKENS];
-    __shared__ int8_t turned[CODES ? 2 : 1][CODES ? COLUMN_TOKENS : 1][ROWS + 4];
+    constexpr int U = COLUMN_UNIT<TYPE>, TOKENS = COLS * U, ROWS = COLUMN_THREADS / COLS, WAVES = COLUMN_THREADS / 64;
+    __shared__ float squares[WAVES][TOKENS], mosts[WAVES][TOKENS], factors[2][TOKENS];
+    __shared__ int8_t turned[CODES ? 2 : 1][CODES ? TOKENS : 1][ROWS + 4];
     const int col = threadIdx.x % COLS, row = threadIdx.x / COLS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t n0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * COLUMN_TOKENS, n = n0 + col * U;
+    const int64_t n0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * TOKENS, n = n0 + col * U;
     if (n0 >= a.tokens) return;
     const int wide = (int)min((int64_t)U, max((int64_t)0, a.tokens - n));
-    float square[U], most[U], held[HELD ? HELD : 1][U];
+    float square[U], most[U], held[HELD][U];
 #pragma unroll
     for (int j = 0; j < U; ++j) square[j] = most[j] = 0.0f;
-    auto weight_of = [&](int64_t k) {
-        float w[1] = {0.0f};
-        if (NORM && k < a.features) load_row_as(a.weight, k, 1, a.weight_type, w);
-        return w[0];
-    };
-    auto look = [&](int64_t k, float (&v)[U]) {
+    float w[HELD][1];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int64_t k = (int64_t)i * ROWS + row;
+        values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, k < a.features ? wide : 0, held[i]);
+        if constexpr (NORM) load_row_as(a.weight, k, k < a.features, a.weight_type, w[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int64_t k = (int64_t)i * ROWS + row;
         if constexpr (NORM)
-            if (a.total.data && k < a.features) store_row<E>(a.total.data, k * a.total.ld + n, wide, v);
-        const float w = NORM && CODES ? weight_of(k) : 1.0f;
+            if (a.total.data && k < a.features) store_row<E>(a.total.data, k * a.total.ld + n, wide, held[i]);
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            if constexpr (NORM) square[j] += v[j] * v[j];
-            if constexpr (NORM && CODES) v[j] *= w;  // p in t's place
-            if constexpr (CODES) most[j] = larger(most[j], v[j]);
-        }
-    };
-    if constexpr (HELD > 0) {
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const int64_t k = (int64_t)i * ROWS + row;
-            values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, k < a.features ? wide : 0, held[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) look((int64_t)i * ROWS + row, held[i]);
-    } else {
-        for (int64_t k = row; k < a.features; k += ROWS) {
-            values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, wide, held[0]);
-            look(k, held[0]);
+            if constexpr (NORM) square[j] += held[i][j] * held[i][j];
+            if constexpr (NORM && CODES) held[i][j] *= w[i][0];  // p in t's place
+            if constexpr (CODES) most[j] = larger(most[j], held[i][j]);
         }
     }
 #pragma unroll
@@ -237,7 +225,7 @@ template <bool NORM, bool CODES, int TYPE, int HELD> __global__ __launch_bounds_
         for (int j = 0; j < U; ++j) squares[wave][lane * U + j] = square[j], mosts[wave][lane * U + j] = most[j];
     }
     __syncthreads();
-    if (threadIdx.x < COLUMN_TOKENS && n0 + threadIdx.x < a.tokens) {  // a thread a token
+    if (threadIdx.x < TOKENS && n0 + threadIdx.x < a.tokens) {  // a thread a token
         float s = squares[0][threadIdx.x], m = mosts[0][threadIdx.x];
         for (int w = 1; w < WAVES; ++w) s += squares[w][threadIdx.x], m = fmaxf(m, mosts[w][threadIdx.x]);
         const token_factors f(NORM, s, m, a);
@@ -249,22 +237,20 @@ template <bool NORM, bool CODES, int TYPE, int HELD> __global__ __launch_bounds_
     float first[U], second[U];  // f, or the two factors of codes
 #pragma unroll
     for (int j = 0; j < U; ++j) first[j] = factors[0][col * U + j], second[j] = factors[1][col * U + j];
-    // (with codes v is p)
-    auto write = [&](int64_t k0, int step, const float (&v)[U]) {
-        const int64_t k = k0 + row;
-        if constexpr (!CODES) {
-            const float w = weight_of(k);
-            float c[U];
 #pragma unroll
-            for (int j = 0; j < U; ++j) c[j] = v[j] * first[j] * w;
-            if (k < a.features) store_row_as(a.out.data, k * a.out.ld + n, wide, a.out.type, c);
+    for (int i = 0; i < HELD; ++i) {
+        const int64_t k0 = (int64_t)i * ROWS, k = k0 + row;
+        if constexpr (!CODES) {
+#pragma unroll
+            for (int j = 0; j < U; ++j) held[i][j] = held[i][j] * first[j] * w[i][0];
+            if (k < a.features) store_row_as(a.out.data, k * a.out.ld + n, wide, a.out.type, held[i]);
         } else {
             // codes change places through LDS: a row of memory is a token there.  Two places in turn, so that one barrier a step is enough.
-            int8_t(&tile)[COLUMN_TOKENS][ROWS + 4] = turned[step & 1];
+            int8_t(&tile)[TOKENS][ROWS + 4] = turned[i & 1];
 #pragma unroll
-            for (int j = 0; j < U; ++j) tile[col * U + j][row] = second[j] == 0.0f ? (int8_t)0 : (int8_t)rintf(v[j] * first[j] * second[j]);
+            for (int j = 0; j < U; ++j) tile[col * U + j][row] = second[j] == 0.0f ? (int8_t)0 : (int8_t)rintf(held[i][j] * first[j] * second[j]);
             __syncthreads();
-            constexpr int EACH = COLUMN_TOKENS * ROWS / COLUMN_THREADS;  // 4 or 8 codes of a token
+            constexpr int EACH = TOKENS * ROWS / COLUMN_THREADS;  // 4 or 8 codes of a token
             const int token = threadIdx.x / (ROWS / EACH), r = threadIdx.x % (ROWS / EACH) * EACH;
             const int there = (int)min((int64_t)EACH, max((int64_t)0, a.features - k0 - r));
             if (n0 + token < a.tokens) {
@@ -276,23 +262,145 @@ template <bool NORM, bool CODES, int TYPE, int HELD> __global__ __launch_bounds_
                 }
             }
         }
-    };
-    if constexpr (HELD > 0) {
+    }
+}
+
+// Otherwise two launches.  A workgroup has a tile of whole pieces of rows: `side` threads of 16 bytes lie side by side (a power of two), 256 / side rows are read at a time.  The
+// first launch leaves every tile's statistics of its tokens, and the sum where it is asked for; in the second every tile adds up those of its tokens, in order, and reads its values again.
+struct column_tiles {
+    int32_t side_bits, rows;  // log2 of side; rows of a tile
+    int64_t across;           // tiles side by side; tiles of a column are gridDim.y
+    float *partial;           // [tile of a column][square, most][tokens]
+};
+
+// (128 bytes of a row side by side; a thread asks for AT_ONCE rows before it looks at the first)
+constexpr int TILE_THREADS = 256, MOST_SIDE_BITS = 3, PIECE_ROWS = 64, AT_ONCE = 4;
+
+template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THREADS) void column_stats_kernel(rows_args a, column_tiles tiles)
+{
+    typedef typename element<TYPE>::type E;
+    constexpr int U = COLUMN_UNIT<TYPE>;
+    __shared__ float squares[4][U << MOST_SIDE_BITS], mosts[4][U << MOST_SIDE_BITS];
+    const int side = 1 << tiles.side_bits, col = threadIdx.x & (side - 1), row = threadIdx.x >> tiles.side_bits, step = TILE_THREADS >> tiles.side_bits;
+    const int64_t n0 = (int64_t)blockIdx.x * side * U, n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
+    const int wide = (int)min((int64_t)U, max((int64_t)0, a.tokens - n));
+    float square[U], most[U];
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) write((int64_t)i * ROWS, i, held[i]);
-    } else {
-        int step = 0;
-        for (int64_t k0 = 0; k0 < a.features; k0 += ROWS, ++step) {
-            const int64_t k = k0 + row;
-            const int there = k < a.features ? wide : 0;
-            if (NORM && a.total.data) load_row<E>(a.total.data, k * a.total.ld + n, there, held[0]);
-            else values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, there, held[0]);
-            if constexpr (NORM && CODES) {
-                const float w = weight_of(k);
+    for (int j = 0; j < U; ++j) square[j] = most[j] = 0.0f;
+    for (int64_t k = k0 + row; k < k1; k += AT_ONCE * step) {
+        float v[AT_ONCE][U];
 #pragma unroll
-                for (int j = 0; j < U; ++j) held[0][j] *= w;
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int64_t at = k + i * step;
+            values_at<NORM, TYPE>(a, at * a.x.ld + n, at * a.y.ld + n, at < k1 ? wide : 0, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int64_t at = k + i * step;
+            float w[1] = {1.0f};
+            if (at >= k1) break;
+            if constexpr (NORM)
+                if (a.total.data) store_row<E>(a.total.data, at * a.total.ld + n, wide, v[i]);
+            if constexpr (NORM && CODES) load_row_as(a.weight, at, 1, a.weight_type, w);
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                if constexpr (NORM) square[j] += v[i][j] * v[i][j];
+                if constexpr (CODES) most[j] = larger(most[j], v[i][j] * w[0]);
             }
-            write(k0, step, held[0]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) reduce_lanes<NORM, CODES>(square[j], most[j], side);
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) < side) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) squares[wave][col * U + j] = square[j], mosts[wave][col * U + j] = most[j];
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < side * U; t += TILE_THREADS) {
+        if (n0 + t >= a.tokens) continue;
+        float *to = tiles.partial + (int64_t)blockIdx.y * 2 * a.tokens + n0 + t;
+        if constexpr (NORM) to[0] = squares[0][t] + squares[1][t] + squares[2][t] + squares[3][t];
+        if constexpr (CODES) to[a.tokens] = fmaxf(fmaxf(mosts[0][t], mosts[1][t]), fmaxf(mosts[2][t], mosts[3][t]));
+    }
+}
+
+template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THREADS) void column_apply_kernel(rows_args a, column_tiles tiles)
+{
+    constexpr int U = COLUMN_UNIT<TYPE>, MOST_TOKENS = U << MOST_SIDE_BITS;
+    __shared__ float sums[2][TILE_THREADS], factors[2][MOST_TOKENS];
+    extern __shared__ int8_t turned[];  // codes: [token][rows of a piece + 4]
+    const int side = 1 << tiles.side_bits, col = threadIdx.x & (side - 1), row = threadIdx.x >> tiles.side_bits, step = TILE_THREADS >> tiles.side_bits, tokens = side * U;
+    const int64_t n0 = (int64_t)blockIdx.x * tokens, n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
+    const int wide = (int)min((int64_t)U, max((int64_t)0, a.tokens - n));
+    // The statistics of this tile's tokens: TILE_THREADS / tokens threads each (tokens is at most TILE_THREADS).
+    {
+        const int t = threadIdx.x & (tokens - 1), token_bits = tiles.side_bits + (U == 4 ? 2 : 3), part = threadIdx.x >> token_bits, parts = TILE_THREADS >> token_bits;
+        float s = 0.0f, m = 0.0f;
+        if (n0 + t < a.tokens) {
+            for (int c = part; c < (int)gridDim.y; c += parts) {
+                const float *from = tiles.partial + (int64_t)c * 2 * a.tokens + n0 + t;
+                if constexpr (NORM) s += from[0];
+                if constexpr (CODES) m = fmaxf(m, from[a.tokens]);
+            }
+        }
+        sums[0][threadIdx.x] = s, sums[1][threadIdx.x] = m;
+        __syncthreads();
+        if (part == 0) {
+            for (int p = 1; p < parts; ++p) s += sums[0][p * tokens + t], m = fmaxf(m, sums[1][p * tokens + t]);
+            const token_factors f(NORM, s, m, a);
+            if (CODES && blockIdx.y == 0 && n0 + t < a.tokens) a.scales[n0 + t] = f.scale;
+            factors[0][t] = CODES ? f.up : f.factor;
+            factors[1][t] = f.steps;
+        }
+        __syncthreads();
+    }
+    float first[U], second[U];  // f, or the two factors of codes
+#pragma unroll
+    for (int j = 0; j < U; ++j) first[j] = factors[0][col * U + j], second[j] = factors[1][col * U + j];
+    auto value = [&](int64_t k, float (&v)[U], float &w) {
+        float weight[1] = {1.0f};
+        values_at<NORM, TYPE>(a, k * a.x.ld + n, k * a.y.ld + n, k < k1 ? wide : 0, v);
+        if constexpr (NORM) load_row_as(a.weight, k, k < k1, a.weight_type, weight);
+        w = weight[0];
+    };
+    if constexpr (!CODES) {
+        for (int64_t k = k0 + row; k < k1; k += AT_ONCE * step) {
+            float v[AT_ONCE][U], w[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) value(k + i * step, v[i], w[i]);
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+#pragma unroll
+                for (int j = 0; j < U; ++j) v[i][j] = v[i][j] * first[j] * w[i];
+                if (k + i * step < k1) store_row_as(a.out.data, (k + i * step) * a.out.ld + n, wide, a.out.type, v[i]);
+            }
+        }
+    } else {
+        // codes change places through LDS, a piece of rows at a time: a row of memory is a token there
+        const int piece = max(step, PIECE_ROWS), pitch = piece + 4;
+        for (int64_t p0 = k0; p0 < k1; p0 += piece) {
+            for (int q = row; q < piece; q += step) {
+                if (p0 + q >= k1) break;
+                float v[U], w;
+                value(p0 + q, v, w);
+#pragma unroll
+                for (int j = 0; j < U; ++j) turned[(col * U + j) * pitch + q] = second[j] == 0.0f ? (int8_t)0 : (int8_t)rintf(v[j] * w * first[j] * second[j]);
+            }
+            __syncthreads();
+            // four codes of a token a thread; pieces are powers of two
+            const int unit_bits = __builtin_ctz(piece) - 2;
+            for (int e = threadIdx.x; e < tokens << unit_bits; e += TILE_THREADS) {
+                const int t = e >> unit_bits, q = (e & ((1 << unit_bits) - 1)) * 4, there = (int)min((int64_t)4, k1 - p0 - q);
+                if (n0 + t >= a.tokens || there <= 0) continue;
+                int8_t *to = reinterpret_cast<int8_t *>(a.out.data) + (n0 + t) * a.out.ld + p0 + q;
+                if (there == 4) {
+                    *reinterpret_cast<neighbours<int8_t, 4> *>(to) = *reinterpret_cast<const neighbours<int8_t, 4> *>(turned + t * pitch + q);
+                } else {
+                    for (int j = 0; j < there; ++j) to[j] = turned[t * pitch + q + j];
+                }
+            }
+            __syncthreads();
         }
     }
 }
@@ -333,14 +441,46 @@ template <int TYPE> hipError_t launch_elements(const rows_args &a, hipStream_t s
     return launch_kernel(elements_kernel<TYPE>, grid_of((rows * units + 255) / 256), 256, 0, stream, a, rows, length, (uint32_t)units);
 }
 
-template <bool NORM, bool CODES, int TYPE> hipError_t launch(const rows_args &a, hipStream_t stream)
+// One launch beats two where a workgroup's registers hold its tokens and few workgroups read the same lines: 0, or the threads side by side.
+int in_one_launch(int64_t K, int64_t N, int unit)
+{
+    if (K <= 4 * COLUMN_THREADS && N <= 32) return 1;
+    return K <= 4 * COLUMN_THREADS / (16 / unit) && N <= 256 ? 16 / unit : 0;
+}
+
+// Tiles of AT_ONCE steps of rows, or as many as leave 64 in a column; whole pieces of codes.
+column_tiles tiles_of(int64_t K, int64_t N, int unit)
+{
+    column_tiles t = {};
+    while (t.side_bits < MOST_SIDE_BITS && (int64_t)unit << t.side_bits < N) ++t.side_bits;
+    const int64_t wide = (int64_t)unit << t.side_bits, step = TILE_THREADS >> t.side_bits, rows = (K + 63) / 64;
+    t.across = (N + wide - 1) / wide;
+    t.rows = (int32_t)((rows + AT_ONCE * step - 1) / (AT_ONCE * step) * (AT_ONCE * step));
+    return t;
+}
+
+template <bool NORM, bool CODES, int TYPE> hipError_t launch(const rows_args &a, char *workspace, hipStream_t stream)
 {
     const int64_t K = a.features, N = a.tokens;
     if (!a.x.by_token) {
-        const dim3 grid = grid_of((N + COLUMN_TOKENS - 1) / COLUMN_TOKENS);
-        if (K <= COLUMN_ROWS<TYPE>) return launch_kernel(columns_kernel<NORM, CODES, TYPE, 1>, grid, COLUMN_THREADS, 0, stream, a);
-        if (K <= 4 * COLUMN_ROWS<TYPE>) return launch_kernel(columns_kernel<NORM, CODES, TYPE, 4>, grid, COLUMN_THREADS, 0, stream, a);
-        return launch_kernel(columns_kernel<NORM, CODES, TYPE, 0>, grid, COLUMN_THREADS, 0, stream, a);
+        auto at_once = [&](auto cols) {
+            constexpr int COLS = decltype(cols)::value, TOKENS = COLS * COLUMN_UNIT<TYPE>, ROWS = COLUMN_THREADS / COLS;
+            const dim3 grid = grid_of((N + TOKENS - 1) / TOKENS);
+            if (K <= ROWS) return launch_kernel(columns_kernel<NORM, CODES, TYPE, COLS, 1>, grid, COLUMN_THREADS, 0, stream, a);
+            return launch_kernel(columns_kernel<NORM, CODES, TYPE, COLS, 4>, grid, COLUMN_THREADS, 0, stream, a);
+        };
+        const int cols = in_one_launch(K, N, COLUMN_UNIT<TYPE>);
+        if (cols == 1) return at_once(std::integral_constant<int, 1>());
+        if (cols > 1) return at_once(std::integral_constant<int, 16 / COLUMN_UNIT<TYPE>>());
+        column_tiles tiles = tiles_of(K, N, COLUMN_UNIT<TYPE>);
+        tiles.partial = reinterpret_cast<float *>(workspace);
+        const dim3 grid((unsigned)tiles.across, (unsigned)((K + tiles.rows - 1) / tiles.rows));
+        const hipError_t e = launch_kernel(column_stats_kernel<NORM, CODES, TYPE>, grid, TILE_THREADS, 0, stream, a, tiles);
+        if (e != hipSuccess) return e;
+        const int step = TILE_THREADS >> tiles.side_bits, piece = step > PIECE_ROWS ? step : PIECE_ROWS;
+        rows_args written = a;  // the sum, where it was written: it may be x's own memory
+        if (a.total.data) written.x = a.total, written.y.data = nullptr;
+        return launch_kernel(column_apply_kernel<NORM, CODES, TYPE>, grid, TILE_THREADS, CODES ? (unsigned)((COLUMN_UNIT<TYPE> << tiles.side_bits) * (piece + 4)) : 0u, stream, written, tiles);
     }
     const int64_t units = (K + UNIT - 1) / UNIT;
     if (units <= 64) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 64, 1, 4>, grid_of((N + 3) / 4), 256, 0, stream, a);
@@ -356,23 +496,30 @@ template <bool NORM, bool CODES, int TYPE> hipError_t launch(const rows_args &a,
     return launch_kernel(long_rows_kernel<NORM, CODES, TYPE>, grid_of(N), 1024, 0, stream, a);
 }
 
-template <int TYPE> hipError_t launch_type(const rows_args &a, bool norm, hipStream_t stream)
+template <int TYPE> hipError_t launch_type(const rows_args &a, bool norm, char *workspace, hipStream_t stream)
 {
     const bool codes = a.out.type == SPMM_I8;
-    if (norm) return codes ? launch<true, true, TYPE>(a, stream) : launch<true, false, TYPE>(a, stream);
-    return codes ? launch<false, true, TYPE>(a, stream) : launch_elements<TYPE>(a, stream);
+    if (norm) return codes ? launch<true, true, TYPE>(a, workspace, stream) : launch<true, false, TYPE>(a, workspace, stream);
+    return codes ? launch<false, true, TYPE>(a, workspace, stream) : launch_elements<TYPE>(a, stream);
 }
 
 }  // namespace
 
-int64_t rows_workspace(const rows_args &, bool) { return 0; }
+int64_t rows_workspace(const rows_args &a, bool norm)
+{
+    if (a.x.by_token || (!norm && a.out.type != SPMM_I8)) return 0;
+    const int unit = a.x.type == SPMM_F32 ? COLUMN_UNIT<SPMM_F32> : COLUMN_UNIT<SPMM_F16>;
+    if (in_one_launch(a.features, a.tokens, unit)) return 0;
+    const column_tiles t = tiles_of(a.features, a.tokens, unit);
+    return (a.features + t.rows - 1) / t.rows * 2 * a.tokens * (int64_t)sizeof(float);
+}
 
-hipError_t rows_launch(const rows_args &a, bool norm, char *, hipStream_t stream)
+hipError_t rows_launch(const rows_args &a, bool norm, char *workspace, hipStream_t stream)
 {
     switch (a.x.type) {
-    case SPMM_F32: return launch_type<SPMM_F32>(a, norm, stream);
-    case SPMM_F16: return launch_type<SPMM_F16>(a, norm, stream);
-    default: return launch_type<SPMM_BF16>(a, norm, stream);
+    case SPMM_F32: return launch_type<SPMM_F32>(a, norm, workspace, stream);
+    case SPMM_F16: return launch_type<SPMM_F16>(a, norm, workspace, stream);
+    default: return launch_type<SPMM_BF16>(a, norm, workspace, stream);
     }
 }
 

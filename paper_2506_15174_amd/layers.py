@@ -48,13 +48,12 @@ def load():
     spec = importlib.util.spec_from_file_location("_spmm_layers", LAYERS_EXT_PATH)
     ext = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(ext)
+    ext.answer_types(Normed, Gated)
     _lib, _ext = lib, ext
     return lib
 
 
 def _on(stream, call, *args):
-    if stream is None:
-        return call(*args)
     import torch
     with torch.cuda.stream(stream):
         return call(*args)
@@ -83,7 +82,10 @@ class QuantPlan:
         C: optional output (M, N), float32, float16 or bfloat16; else allocated in `dtype` (B's type; float32 for
         codes) and in B's order.  Returns C.
         """
-        C = _on(stream, _ext.quant_execute, self._address, self._M, self._K, B, C, scales, dtype)
+        if stream is None:
+            C = _ext.quant_execute(self._address, self._M, self._K, B, C, scales, dtype)
+        else:
+            C = _on(stream, _ext.quant_execute, self._address, self._M, self._K, B, C, scales, dtype)
         if type(C) is int:
             raise SpmmError(C, "spmm_quant_execute")
         return C
@@ -150,10 +152,13 @@ def norm(x, weight, eps=1e-6, residual=None, total=None, out=None, scales=None, 
     """
     if _ext is None:
         load()
-    res = _on(stream, _ext.norm, x, weight, eps, residual, total, residual is not None, out, scales, dtype)
+    if stream is None:
+        res = _ext.norm(x, weight, eps, residual, total, residual is not None, out, scales, dtype)
+    else:
+        res = _on(stream, _ext.norm, x, weight, eps, residual, total, residual is not None, out, scales, dtype)
     if type(res) is int:
         raise SpmmError(res, "spmm_norm")
-    return Normed(*res)
+    return res
 
 
 def gate(a, b=None, act="silu", out=None, scales=None, dtype=None, stream=None):
@@ -165,7 +170,10 @@ def gate(a, b=None, act="silu", out=None, scales=None, dtype=None, stream=None):
         raise ValueError("act must be one of %s" % ", ".join(sorted(ACTS)))
     if _ext is None:
         load()
-    res = _on(stream, _ext.gate, a, b, ACTS[act], out, scales, dtype)
+    if stream is None:
+        res = _ext.gate(a, b, ACTS[act], out, scales, dtype)
+    else:
+        res = _on(stream, _ext.gate, a, b, ACTS[act], out, scales, dtype)
     if type(res) is int:
         raise SpmmError(res, "spmm_gate")
-    return Gated(*res)
+    return res
