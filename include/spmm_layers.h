@@ -68,10 +68,10 @@ spmm_status_t spmm_quant_describe(const spmm_quant_t *plan, int64_t *M, int64_t 
                                   int64_t *device_bytes);
 
 /*
- * Bytes of DEVICE memory that spmm_quant_execute needs as its workspace for N columns of B in the given type
- * (whatever their order); 0: none.
+ * Bytes of DEVICE memory that spmm_quant_execute needs as its workspace for N columns of a B of this type and
+ * memory order (data is not read); 0: none, as always up to 16 columns.
  */
-spmm_status_t spmm_quant_workspace(const spmm_quant_t *plan, int32_t B_type, int64_t N, size_t *bytes);
+spmm_status_t spmm_quant_workspace(const spmm_quant_t *plan, const spmm_tensor_t *B, int64_t N, size_t *bytes);
 
 /*
  * C <- W x B.

@@ -42,7 +42,7 @@ struct tensor {
 };
 
 // Bytes of B laid out for the product, and the launches.
-int64_t quant_workspace(const quant_matrix &w, int32_t type, int64_t N);
+int64_t quant_workspace(const quant_matrix &w, const tensor &B, int64_t N);
 hipError_t quant_execute(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, char *workspace, hipStream_t stream);
 
 // ---- norm and gate -------------------------------------------------------------------------------------------

@@ -287,6 +287,19 @@ spmm_status_t run_rows(const rows_args &a, bool norm, void *workspace, size_t by
     return status_of(rows_launch(a, norm, static_cast<char *>(workspace), static_cast<hipStream_t>(stream)));
 }
 
+// B of the product.  Without columns of W there is nothing to look at.
+spmm_status_t seen_operand(const quant_matrix &w, const spmm_tensor_t *B, int64_t N, tensor *b)
+{
+    if (!B || B->type < SPMM_F32 || B->type > SPMM_I8) return SPMM_ERR_INVALID_ARG;
+    *b = {nullptr, 1, B->type, true};
+    if (w.K == 0) return SPMM_OK;
+    const spmm_status_t st = seen(*B, w.K, N, b);
+    if (st != SPMM_OK || b->type != SPMM_I8 || b->by_token) return st;
+    if (w.K != 1 || b->ld != N) return SPMM_ERR_UNSUPPORTED;
+    *b = {b->data, 1, SPMM_I8, true};
+    return SPMM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -314,11 +327,13 @@ spmm_status_t spmm_quant_describe(const spmm_quant_t *plan, int64_t *M, int64_t 
     return SPMM_OK;
 }
 
-spmm_status_t spmm_quant_workspace(const spmm_quant_t *plan, int32_t B_type, int64_t N, size_t *bytes)
+spmm_status_t spmm_quant_workspace(const spmm_quant_t *plan, const spmm_tensor_t *B, int64_t N, size_t *bytes)
 {
-    if (!plan || !bytes || B_type < SPMM_F32 || B_type > SPMM_I8 || N < 1 || N > MOST_EXTENT) return SPMM_ERR_INVALID_ARG;
-    *bytes = (size_t)quant_workspace(plan->w, B_type, N);
-    return SPMM_OK;
+    if (!plan || !bytes || N < 1 || N > MOST_EXTENT) return SPMM_ERR_INVALID_ARG;
+    tensor b = {};
+    const spmm_status_t st = seen_operand(plan->w, B, N, &b);
+    if (st == SPMM_OK) *bytes = (size_t)quant_workspace(plan->w, b, N);
+    return st;
 }
 
 spmm_status_t spmm_quant_execute(const spmm_quant_t *plan, const spmm_tensor_t *B, const float *B_scales, int64_t N, const spmm_tensor_t *C, void *workspace,
@@ -331,22 +346,15 @@ spmm_status_t spmm_quant_execute(const spmm_quant_t *plan, const spmm_tensor_t *
         (void)hipGetLastError();
         return SPMM_ERR_INVALID_ARG;
     }
-    if (B->type < SPMM_F32 || B->type > SPMM_I8 || C->type < SPMM_F32 || C->type > SPMM_BF16) return SPMM_ERR_INVALID_ARG;
-    if (w.M == 0) return SPMM_OK;
+    if (C->type < SPMM_F32 || C->type > SPMM_BF16) return SPMM_ERR_INVALID_ARG;
     tensor b = {}, c = {};
-    spmm_status_t st = SPMM_OK;
-    if (w.K > 0 && (st = seen(*B, w.K, N, &b)) != SPMM_OK) return st;
-    if (w.K == 0) b.type = B->type;
+    spmm_status_t st = seen_operand(w, B, N, &b);
+    if (st != SPMM_OK) return st;
+    if (b.type == SPMM_I8 && (!B_scales || (uintptr_t)B_scales % 4 != 0)) return SPMM_ERR_INVALID_ARG;
+    if (w.M == 0) return SPMM_OK;
     if ((st = seen(*C, w.M, N, &c)) != SPMM_OK) return st;
-    if (b.type == SPMM_I8) {
-        if (!B_scales || (uintptr_t)B_scales % 4 != 0) return SPMM_ERR_INVALID_ARG;
-        if (w.K > 0 && !b.by_token) {
-            if (w.K != 1 || b.ld != N) return SPMM_ERR_UNSUPPORTED;
-            b = {b.data, 1, SPMM_I8, true};
-        }
-    }
     if (meet(span_of(b, w.K, N), span_of(c, w.M, N))) return SPMM_ERR_INVALID_ARG;
-    if (!room(workspace, workspace_bytes, quant_workspace(w, b.type, N))) return SPMM_ERR_INVALID_ARG;
+    if (!room(workspace, workspace_bytes, quant_workspace(w, b, N))) return SPMM_ERR_INVALID_ARG;
     return status_of(quant_execute(w, b, b.type == SPMM_I8 ? B_scales : nullptr, N, c, static_cast<char *>(workspace), static_cast<hipStream_t>(stream)));
 }
 

@@ -260,7 +260,7 @@ PyObject *quant_execute(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             const spmm_tensor_t c = {C.data_ptr(), C.stride(0), C.stride(1), type_of(C.scalar_type())};
             size_t bytes = 0;
             workspace room;
-            st = spmm_quant_workspace(plan, b.type, N, &bytes);
+            st = spmm_quant_workspace(plan, &b, N, &bytes);
             if (st == SPMM_OK) {
                 room.take(bytes, from);
                 st = spmm_quant_execute(plan, &b, scales ? static_cast<const float *>(scales->data_ptr()) : nullptr, N, &c, room.data, room.bytes, stream_beside(*B));

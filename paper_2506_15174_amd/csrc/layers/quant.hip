@@ -33,7 +33,8 @@ template <int BT> constexpr int PARTS = BT == SPMM_F32 ? 3 : 1;
 // Bytes of one part of 16 tokens x 32 columns.
 template <int BT> constexpr int STEP_BYTES = BT == SPMM_I8 ? 512 : 1024;
 
-constexpr int WAVES = 8;
+// A launch has at most 65535 workgroups along its second axis, of four tiles of tokens or fewer.
+constexpr int64_t MOST_TOKEN_TILES = 65535 / 8 * 8;
 
 // ---- B as the instructions take it ---------------------------------------------------------------------------
 //
@@ -555,20 +556,20 @@ template <int BT, int ROW_WAVES, int TOKEN_WAVES, int STEPS, bool ZEROS> __globa
 
 template <int V> using constant = std::integral_constant<int, V>;
 
-// ---- few tokens ------------------------------------------------------------------------------------------------
+// ---- in one launch ---------------------------------------------------------------------------------------------
 //
-// Up to 16 tokens are one tile, and a product is over in the time of a few memory accesses: one launch, in which every wave reads its columns of
+// A product of few tokens is over in the time of a few memory accesses, of which a launch is two or three: every wave reads its columns of
 // B as it reads its weights and makes operands of them itself.  Lanes of tokens that do not exist read the last one's (an access the
 // wave makes anyway); their results are not stored.  Weights, scales and B of AHEAD blocks are asked for before the first is used.
 //   PER_GROUP  steps of 32 columns behind which a group's sum is full (4, 2 or 1)
-//   RT         tiles of rows of a wave, which share its operands of B
+//   RT, NT     tiles of rows and of tokens of a wave
 //   FMA        one token in fp32 is multiplied by ordinary instructions, a lane a row and a quarter of the columns: making three parts of a value
 //              takes six
 //   KWAVES     waves of a workgroup, which share K
 
-template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, bool FMA, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void few_kernel(quant_matrix W, tensor B, const float *B_scales, int32_t N, tensor C)
+template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int AHEAD, bool FMA, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void direct_kernel(quant_matrix W, tensor B, const float *B_scales, int64_t N, tensor C)
 {
-    __shared__ float sums[KWAVES][RT][256];
+    __shared__ float sums[KWAVES][RT][NT][256], token_scales[BT == SPMM_I8 ? 16 * NT : 1];
     constexpr int SUMS = 4 / PER_GROUP;
     constexpr int64_t SIZE = sizeof(typename stored<BT>::type);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
@@ -577,11 +578,15 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
     const int64_t tile0 = (int64_t)blockIdx.x * RT;
     const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
     const int64_t column = (BY_TOKEN ? 1 : B.ld) * SIZE;  // bytes from one to the next
-    const char *const token = B.data + (FMA ? 0 : min(r, N - 1)) * (BY_TOKEN ? B.ld : 1) * SIZE, *const mine = token + 8 * q * column;
+    const int64_t n0 = (int64_t)blockIdx.y * (16 * NT);
+    const char *token[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) token[t] = B.data + (FMA ? 0 : min(n0 + 16 * t + r, N - 1)) * (BY_TOKEN ? B.ld : 1) * SIZE;
+    if (BT == SPMM_I8 && threadIdx.x < 16 * NT) token_scales[threadIdx.x] = B_scales[min(n0 + (int64_t)threadIdx.x, N - 1)];
     struct asked {
         u32x4 word[RT];
         span_values<SUMS, ZEROS> span[RT];
-        raw<BT> b[4];
+        raw<BT> b[NT][4];
     };
     auto ask = [&](int b, asked &a, auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
@@ -589,19 +594,18 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
         for (int i = 0; i < RT; ++i) a.word[i] = reinterpret_cast<const u32x4 *>(codes + ((int64_t)i * W.blocks + b) * BLOCK_WORDS)[lane];
         const int left = (int)(W.K - (int64_t)b * BLOCK_COLS);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) a.b[s] = fetch<BT, BY_TOKEN, TAIL>((TAIL ? token : mine) + b * BLOCK_COLS * column, column, 32 * s + (TAIL ? 8 * q : 0), left);
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) a.b[t][s] = fetch<BT, BY_TOKEN, TAIL>(token[t] + (b * BLOCK_COLS + (TAIL ? 0 : 8 * q)) * column, column, 32 * s + (TAIL ? 8 * q : 0), left);
 #pragma unroll
         for (int i = 0; i < RT; ++i) a.span[i] = span_of<SUMS, ZEROS>(W, tile0 + i, b, r);
     };
-    f32x4 acc[RT];
+    f32x4 acc[RT][NT];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) acc[i] = f32x4{0, 0, 0, 0};
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
     auto use = [&](const asked &a) {
-        operands<BT> o[4];
-        if constexpr (!FMA) {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) o[s] = operands_of<BT>(a.b[s]);
-        }
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             // (one tile's weights at a time: the registers do not hold all of them as operands)
@@ -614,44 +618,60 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
                     __builtin_amdgcn_sched_barrier(0);
                     weights_f32<ZEROS>(a.word[i][s], a.span[i].zero(s / PER_GROUP), w);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) part = __builtin_fmaf(w[j], a.b[s].v[j], part);
-                    if (s % PER_GROUP == PER_GROUP - 1) acc[i][0] += a.span[i].scale[s / PER_GROUP] * WEIGHT_UNIT<BT> * part, part = 0.0f;
+                    for (int j = 0; j < 8; ++j) part = __builtin_fmaf(w[j], a.b[0][s].v[j], part);
+                    if (s % PER_GROUP == PER_GROUP - 1) acc[i][0][0] += a.span[i].scale[s / PER_GROUP] * WEIGHT_UNIT<BT> * part, part = 0.0f;
                 }
-            } else if constexpr (BT == SPMM_I8) {
-                u32x2 w[4];
+                continue;
+            }
+            u32x4 w[4];  // codes: two steps in one
 #pragma unroll
-                for (int s = 0; s < 4; ++s) w[s] = weights_i8(a.word[i][s], a.span[i].zero(s / PER_GROUP) * 0x01010101u);
-                i32x4 part;
-#pragma unroll
-                for (int s = 0; s < 4; s += PER_GROUP == 1 ? 1 : 2) {
-                    const bool begins = s % PER_GROUP == 0;
-                    if constexpr (PER_GROUP == 1) {
-                        part = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, o[s].part[0]), __builtin_bit_cast(long, w[s]), i32x4{0, 0, 0, 0}, 0, 0, 0);
-                    } else {
-                        const i32x4 x = {(int)o[s].part[0][0], (int)o[s].part[0][1], (int)o[s + 1].part[0][0], (int)o[s + 1].part[0][1]};
-                        const i32x4 y = {(int)w[s][0], (int)w[s][1], (int)w[s + 1][0], (int)w[s + 1][1]};
-                        part = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, begins ? i32x4{0, 0, 0, 0} : part, 0, 0, 0);
-                    }
-                    if (PER_GROUP < 4 || s == 2) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][e] += a.span[i].scale[s / PER_GROUP] * (float)part[e];
-                    }
+            for (int s = 0; s < 4; ++s) {
+                const int zero = a.span[i].zero(s / PER_GROUP);
+                if constexpr (BT == SPMM_I8) {
+                    const u32x2 v = weights_i8(a.word[i][s], (uint32_t)zero * 0x01010101u);
+                    w[s / 2][2 * (s % 2)] = v[0], w[s / 2][2 * (s % 2) + 1] = v[1];
+                } else if constexpr (BT == SPMM_F16) {
+                    w[s] = __builtin_bit_cast(u32x4, weights_f16(a.word[i][s], zero));
+                } else {
+                    w[s] = __builtin_bit_cast(u32x4, weights_bf16<ZEROS>(a.word[i][s], zero));
                 }
-            } else {
-                f32x4 part;
+            }
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    if (s % PER_GROUP == 0) part = f32x4{0, 0, 0, 0};
-                    if constexpr (BT == SPMM_F16) {
-                        part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, o[s].part[0]), weights_f16(a.word[i][s], a.span[i].zero(s / PER_GROUP)), part, 0, 0, 0);
-                    } else {
-                        const bf16x8 w = weights_bf16<ZEROS>(a.word[i][s], a.span[i].zero(s / PER_GROUP));
+            for (int t = 0; t < NT; ++t) {
+                if (BT == SPMM_F32 && NT > 1) __builtin_amdgcn_sched_barrier(0);  // (nor three parts of two tiles of tokens)
+                if constexpr (BT == SPMM_I8) {
+                    i32x4 part;
 #pragma unroll
-                        for (int p = PARTS<BT> - 1; p >= 0; --p) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o[s].part[p]), w, part, 0, 0, 0);
+                    for (int s = 0; s < 4; s += PER_GROUP == 1 ? 1 : 2) {
+                        const u32x2 x0 = operands_of<BT>(a.b[t][s]).part[0];
+                        if constexpr (PER_GROUP == 1) {
+                            const int h = 2 * (s % 2);
+                            part = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, x0), (long)((uint64_t)w[s / 2][h] | (uint64_t)w[s / 2][h + 1] << 32), i32x4{0, 0, 0, 0}, 0, 0, 0);
+                        } else {
+                            const u32x2 x1 = operands_of<BT>(a.b[t][s + 1]).part[0];
+                            const i32x4 x = {(int)x0[0], (int)x0[1], (int)x1[0], (int)x1[1]};
+                            part = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, __builtin_bit_cast(i32x4, w[s / 2]), s % PER_GROUP == 0 ? i32x4{0, 0, 0, 0} : part, 0, 0, 0);
+                        }
+                        if (PER_GROUP < 4 || s == 2) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][t][e] += a.span[i].scale[s / PER_GROUP] * (float)part[e];
+                        }
                     }
-                    if (s % PER_GROUP == PER_GROUP - 1) {
+                } else {
+                    f32x4 part;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][e] += a.span[i].scale[s / PER_GROUP] * WEIGHT_UNIT<BT> * part[e];
+                    for (int s = 0; s < 4; ++s) {
+                        const operands<BT> o = operands_of<BT>(a.b[t][s]);
+                        if (s % PER_GROUP == 0) part = f32x4{0, 0, 0, 0};
+#pragma unroll
+                        for (int p = PARTS<BT> - 1; p >= 0; --p) {
+                            if constexpr (BT == SPMM_F16) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, o.part[p]), __builtin_bit_cast(f16x8, w[s]), part, 0, 0, 0);
+                            else part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o.part[p]), __builtin_bit_cast(bf16x8, w[s]), part, 0, 0, 0);
+                        }
+                        if (s % PER_GROUP == PER_GROUP - 1) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][t][e] += a.span[i].scale[s / PER_GROUP] * WEIGHT_UNIT<BT> * part[e];
+                        }
                     }
                 }
             }
@@ -678,44 +698,53 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int KWAVES, int AHEAD, b
     if constexpr (FMA) {  // the four quarters of the columns
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            acc[i][0] += __shfl_xor(acc[i][0], 16);
-            acc[i][0] += __shfl_xor(acc[i][0], 32);
+            acc[i][0][0] += __shfl_xor(acc[i][0][0], 16);
+            acc[i][0][0] += __shfl_xor(acc[i][0][0], 32);
         }
     }
 #pragma unroll
-    for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4 *>(&sums[wave][i][lane * 4]) = acc[i];
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(&sums[wave][i][t][lane * 4]) = acc[i][t];
     __syncthreads();
     // the waves' sums, in wave order: a thread an element of C
-    for (int e = threadIdx.x; e < RT * 256; e += 64 * KWAVES) {
-        const int m = C.by_token ? e % (16 * RT) : e / 16, t = C.by_token ? e / (16 * RT) : e % 16;
-        const int64_t row = tile0 * TILE_ROWS + m;
-        if (row >= W.M || t >= N) continue;
-        const int at = (t >> 2) * 64 + (m % 16) * 4 + (t & 3);
+    for (int e = threadIdx.x; e < RT * NT * 256; e += 64 * KWAVES) {
+        const int m = C.by_token ? e % (16 * RT) : e / (16 * NT), t = C.by_token ? e / (16 * RT) : e % (16 * NT);
+        const int64_t row = tile0 * TILE_ROWS + m, n = n0 + t;
+        if (row >= W.M || n >= N) continue;
+        const int at = ((t & 15) >> 2) * 64 + (m % 16) * 4 + (t & 3);
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < KWAVES; ++w) v += sums[w][m / 16][at];
-        if (BT == SPMM_I8) v *= B_scales[t];
-        store_as(C.data, C.by_token ? t * C.ld + row : row * C.ld + t, C.type, v);
+        for (int w = 0; w < KWAVES; ++w) v += sums[w][m / 16][t / 16][at];
+        if (BT == SPMM_I8) v *= token_scales[t];
+        store_as(C.data, C.by_token ? n * C.ld + row : row * C.ld + n, C.type, v);
     }
 }
 
-template <int BT, bool BY_TOKEN, bool FMA> hipError_t execute_few(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
+// Token by token of fp32 by multiply-adds, else on the matrix cores.  Tiles: a wave has more where workgroups are left over otherwise (256 compute units).
+template <int BT, bool BY_TOKEN, bool FMA> hipError_t execute_direct(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
-    auto shaped = [&](auto per_group, auto rt, auto kwaves, auto ahead) {
-        constexpr int PER_GROUP = decltype(per_group)::value, RT = decltype(rt)::value, KWAVES = decltype(kwaves)::value, AHEAD = decltype(ahead)::value;
-        const dim3 blocks((unsigned)((w.tiles + RT - 1) / RT));
-        if (w.zeros) return launch_kernel(few_kernel<BT, BY_TOKEN, PER_GROUP, RT, KWAVES, AHEAD, FMA, true>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, (int32_t)N, C);
-        return launch_kernel(few_kernel<BT, BY_TOKEN, PER_GROUP, RT, KWAVES, AHEAD, FMA, false>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, (int32_t)N, C);
+    auto shaped = [&](auto per_group, auto rt, auto nt, auto kwaves, auto ahead) {
+        constexpr int PER_GROUP = decltype(per_group)::value, RT = decltype(rt)::value, NT = decltype(nt)::value, KWAVES = decltype(kwaves)::value, AHEAD = decltype(ahead)::value;
+        const dim3 blocks((unsigned)((w.tiles + RT - 1) / RT), (unsigned)((N + 16 * NT - 1) / (16 * NT)));
+        if (w.zeros) return launch_kernel(direct_kernel<BT, BY_TOKEN, PER_GROUP, RT, NT, KWAVES, AHEAD, FMA, true>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, N, C);
+        return launch_kernel(direct_kernel<BT, BY_TOKEN, PER_GROUP, RT, NT, KWAVES, AHEAD, FMA, false>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, N, C);
     };
     auto run = [&](auto per_group) {
+        constexpr int PER_GROUP = decltype(per_group)::value;
+        if constexpr (!FMA) {
+            if (N > 16) {
+                return shaped(per_group, constant<1>(), constant<2>(), constant<8>(), constant<1>());
+            }
+        }
         // (what the registers hold)
-        constexpr int AHEAD = BT == SPMM_F32 && !FMA ? 1 : 2, LESS = decltype(per_group)::value < 4 || FMA ? 1 : AHEAD;
-        constexpr int MOST = decltype(per_group)::value == 1 || (BT == SPMM_F32 && !BY_TOKEN) ? 2 : 4;
-        if (w.tiles >= 1024) return shaped(per_group, constant<MOST>(), constant<8>(), constant<LESS>());
-        if (w.tiles >= 512) return shaped(per_group, constant<2>(), constant<8>(), constant<AHEAD>());
+        constexpr int AHEAD = BT == SPMM_F32 && !FMA ? 1 : 2, LESS = PER_GROUP < 4 || FMA ? 1 : AHEAD;
+        constexpr int MOST = PER_GROUP == 1 || (BT == SPMM_F32 && !BY_TOKEN) ? 2 : 4;
+        if (w.tiles >= 1024) return shaped(per_group, constant<MOST>(), constant<1>(), constant<8>(), constant<LESS>());
+        if (w.tiles >= 512) return shaped(per_group, constant<2>(), constant<1>(), constant<8>(), constant<AHEAD>());
         if constexpr (BY_TOKEN && BT != SPMM_F32)
-            if (w.blocks > 8) return shaped(per_group, constant<1>(), constant<16>(), constant<LESS>());
-        return shaped(per_group, constant<1>(), constant<8>(), constant<1>());
+            if (w.blocks > 8) return shaped(per_group, constant<1>(), constant<1>(), constant<16>(), constant<LESS>());
+        return shaped(per_group, constant<1>(), constant<1>(), constant<8>(), constant<1>());
     };
     if (w.group == 32) return run(constant<1>());
     if (w.group == 64) return run(constant<2>());
@@ -752,31 +781,50 @@ template <int BT, int ROW_WAVES, int TOKEN_WAVES> hipError_t launch_wide(const q
     return run(constant<4>());
 }
 
+// On B laid out by pack_kernel.  Small tiles while they leave no compute unit without a workgroup; then larger ones, which read B and make operands of weights less often.
+// us, tiles of rows x of tokens of a wave (wide: wide_kernel), bf16:
+//   1024 x 4096, 128 tokens   1x2  9.4   2x2 10.8   2x4 13.2                 4096 x 4096, 128   1x2 17.0   2x2 14.7   2x4 14.0
+//   16384 x 4096, 64          1x2 33     2x2 26     2x4 27                   3001 x 2511, 200   1x2 15.5   2x2 14.8   2x4 18.8
+//   8192 x 8192, 256          2x2 70     2x4 67     wide 60                  8192 x 4096, 320   2x2 50     2x4 54     wide 58 (320 workgroups)
+// in codes: 8192 x 8192, 256 2x2 53, 4x4 41; 2048 x 8192, 512 2x2 28, 4x4 35 (256 workgroups)
+// in fp32: 4096 x 4096, 128 2x2 26, 2x4 23, 4x4 34; 4096 x 4096, 256 2x2 47, 2x4 42, 4x4 36
 template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
-    if (N <= 32) return launch_many<BT, 2, 1, 8>(w, B, B_scales, N, C, stream);
-    if (N <= 64) return launch_many<BT, 4, 1, 8>(w, B, B_scales, N, C, stream);
-    // workgroups of 128 rows and 128 tokens (fp32: 64), of which the chip should be full
-    constexpr int64_t WIDE_TOKENS = 32 * WIDE_NT<BT>;
-    if ((w.tiles + 7) / 8 * ((N + WIDE_TOKENS - 1) / WIDE_TOKENS) >= 200) return launch_wide<BT, 2, 2>(w, B, B_scales, N, C, stream);
-    const int64_t columns = (N + 127) / 128;
-    if ((w.tiles + 3) / 4 * columns >= 192) return launch_many<BT, 8, 4, 4>(w, B, B_scales, N, C, stream);
-    return launch_many<BT, 8, 1, 8>(w, B, B_scales, N, C, stream);
+    auto workgroups = [&](int64_t rows, int64_t tokens) { return (w.tiles + rows - 1) / rows * ((N + 16 * tokens - 1) / (16 * tokens)); };
+    if (workgroups(1, 2) <= 256) return launch_many<BT, 2, 1, 8>(w, B, B_scales, N, C, stream);
+    if constexpr (BT == SPMM_F32) {
+        if (workgroups(4, 4) >= 180) return launch_many<BT, 4, 4, 4>(w, B, B_scales, N, C, stream);
+        if (workgroups(2, 4) >= 180) return launch_many<BT, 4, 2, 8>(w, B, B_scales, N, C, stream);
+    } else if constexpr (BT == SPMM_I8) {
+        if (workgroups(4, 4) >= 480) return launch_many<BT, 4, 4, 4>(w, B, B_scales, N, C, stream);
+    } else {
+        const int64_t wide = workgroups(8, 4), rounds = (wide + 255) / 256;
+        if (w.K >= 4096 && wide * 10 >= rounds * 256 * 9) return launch_wide<BT, 2, 1>(w, B, B_scales, N, C, stream);
+    }
+    return launch_many<BT, 2, 2, 8>(w, B, B_scales, N, C, stream);
+}
+
+// Whether a product goes in one launch.  Up to 16 tokens always.  With more, lanes read B in pieces of 16 bytes of as many rows of memory, which many_kernel reads from the laid out
+// B in pieces of 1 KiB, and only what a launch costs speaks for it: where each wave has one block of columns and each compute unit one workgroup.
+// us in one launch and in two, bf16: 4096 x 1024, 32 tokens 4.2 and 5.0; 4096 x 2048 6.4 and 6.5; 4096 x 4096 10.0 and 8.5; 16384 x 1024 14 and 7.6.
+// fp32 by features: 4096 x 1024, 32 tokens 6.7 and 7.2; 4096 x 2048 9.9 and 9.5.
+bool is_direct(const quant_matrix &w, int64_t N)
+{
+    return N <= 16 || (N <= 128 && w.blocks <= 8 && w.tiles * ((N + 31) / 32) <= 256);
 }
 
 template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, char *workspace, hipStream_t stream)
 {
-    if (N <= 16) {
+    if (is_direct(w, N)) {
         if constexpr (BT == SPMM_F32)
-            if (B.by_token && N == 1) return execute_few<BT, true, true>(w, B, B_scales, N, C, stream);
-        if (B.by_token) return execute_few<BT, true, false>(w, B, B_scales, N, C, stream);
-        if constexpr (BT != SPMM_I8) return execute_few<BT, false, false>(w, B, B_scales, N, C, stream);
+            if (B.by_token && N == 1) return execute_direct<BT, true, true>(w, B, B_scales, N, C, stream);
+        if (B.by_token) return execute_direct<BT, true, false>(w, B, B_scales, N, C, stream);
+        if constexpr (BT != SPMM_I8) return execute_direct<BT, false, false>(w, B, B_scales, N, C, stream);
     }
-    const int64_t token_tiles = (N + 15) / 16;
     // a launch of each for 2^16 - 1 tiles of tokens at a time
-    constexpr int64_t MOST = 65535 / 8 * 8;
-    for (int64_t t0 = 0; t0 < token_tiles; t0 += MOST) {
-        const int64_t tiles = token_tiles - t0 < MOST ? token_tiles - t0 : MOST, n0 = t0 * 16, n = N - n0 < tiles * 16 ? N - n0 : tiles * 16;
+    const int64_t token_tiles = (N + 15) / 16;
+    for (int64_t t0 = 0; t0 < token_tiles; t0 += MOST_TOKEN_TILES) {
+        const int64_t tiles = token_tiles - t0 < MOST_TOKEN_TILES ? token_tiles - t0 : MOST_TOKEN_TILES, n0 = t0 * 16, n = N - n0 < tiles * 16 ? N - n0 : tiles * 16;
         const int64_t size = BT == SPMM_I8 ? 1 : BT == SPMM_F32 ? 4 : 2, c_size = C.type == SPMM_F32 ? 4 : 2;
         tensor b = B, c = C;
         b.data += n0 * (B.by_token ? B.ld : 1) * size;
@@ -795,12 +843,11 @@ template <int BT> hipError_t execute(const quant_matrix &w, const tensor &B, con
 
 }  // namespace
 
-int64_t quant_workspace(const quant_matrix &w, int32_t type, int64_t N)
+int64_t quant_workspace(const quant_matrix &w, const tensor &B, int64_t N)
 {
-    if (N <= 16) return 0;
-    const int64_t step = type == SPMM_F32 ? 3 * 1024 : type == SPMM_I8 ? 512 : 1024, tiles = (N + 15) / 16;
-    const int64_t most = 65535 / 8 * 8;
-    return (tiles < most ? tiles : most) * w.blocks * 4 * step;
+    if (is_direct(w, N)) return 0;
+    const int64_t step = B.type == SPMM_F32 ? 3 * 1024 : B.type == SPMM_I8 ? 512 : 1024, tiles = (N + 15) / 16;
+    return (tiles < MOST_TOKEN_TILES ? tiles : MOST_TOKEN_TILES) * w.blocks * 4 * step;
 }
 
 hipError_t quant_execute(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, char *workspace, hipStream_t stream)

@@ -47,7 +47,7 @@ void operator delete(void *p, size_t) noexcept { free(p); }
 
 static layers::quant_matrix last_matrix;
 namespace layers {
-int64_t quant_workspace(const quant_matrix &, int32_t, int64_t) { return 64; }
+int64_t quant_workspace(const quant_matrix &, const tensor &, int64_t) { return 64; }
 hipError_t quant_execute(const quant_matrix &w, const tensor &B, const float *, int64_t, const tensor &C, char *, hipStream_t)
 {
     ++launches;
@@ -157,10 +157,14 @@ static void product_refusals()
     CHECK(spmm_quant_create(&plan, 5, 10, 32, codes, scales, zeros) == SPMM_OK);
     const spmm_tensor_t b = {B, 3, 1, SPMM_F32}, c = {C, 3, 1, SPMM_F32};
     size_t bytes = 0;
-    CHECK(spmm_quant_workspace(plan, SPMM_F32, 3, &bytes) == SPMM_OK && bytes == 64);
-    for (int type : {-1, 4}) CHECK(spmm_quant_workspace(plan, type, 3, &bytes) == SPMM_ERR_INVALID_ARG);
+    CHECK(spmm_quant_workspace(plan, &b, 3, &bytes) == SPMM_OK && bytes == 64);
+    for (int type : {-1, 4}) {
+        const spmm_tensor_t bad = {B, 3, 1, type};
+        CHECK(spmm_quant_workspace(plan, &bad, 3, &bytes) == SPMM_ERR_INVALID_ARG);
+    }
+    CHECK(spmm_quant_workspace(plan, nullptr, 3, &bytes) == SPMM_ERR_INVALID_ARG && spmm_quant_workspace(plan, &b, 3, nullptr) == SPMM_ERR_INVALID_ARG);
     for (int64_t N : {(int64_t)0, (int64_t)-1, (int64_t)1 << 31}) {
-        CHECK(spmm_quant_workspace(plan, SPMM_F32, N, &bytes) == SPMM_ERR_INVALID_ARG);
+        CHECK(spmm_quant_workspace(plan, &b, N, &bytes) == SPMM_ERR_INVALID_ARG);
         CHECK(spmm_quant_execute(plan, &b, nullptr, N, &c, room, 64, nullptr) == SPMM_ERR_INVALID_ARG);
     }
     launches = 0;
