@@ -176,10 +176,10 @@ __device__ inline f16x8 weights_f16(uint32_t w, int zero)
 {
     const _Float16 z = (_Float16)(float)(1024 + zero);
     const f16x2 base = {z, z};
-    f16x2 v[4];
+    uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) ^ 0x64086408u) - base;
-    return __builtin_bit_cast(f16x8, *reinterpret_cast<u32x4 *>(v));
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) ^ 0x64086408u) - base);
+    return __builtin_bit_cast(f16x8, u32x4{v[0], v[1], v[2], v[3]});
 }
 
 // (code - 8) / 16 of the low nibble of byte I, which the hardware has an instruction for.
@@ -567,7 +567,7 @@ template <int V> using constant = std::integral_constant<int, V>;
 //              takes six
 //   KWAVES     waves of a workgroup, which share K
 
-template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int AHEAD, bool FMA, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void direct_kernel(quant_matrix W, tensor B, const float *B_scales, int64_t N, tensor C)
+template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int AHEAD, bool FMA, bool STAGED, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void direct_kernel(quant_matrix W, tensor B, const float *B_scales, int64_t N, tensor C)
 {
     __shared__ float sums[KWAVES][RT][NT][256], token_scales[BT == SPMM_I8 ? 16 * NT : 1];
     constexpr int SUMS = 4 / PER_GROUP;
@@ -583,16 +583,30 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
 #pragma unroll
     for (int t = 0; t < NT; ++t) token[t] = B.data + (FMA ? 0 : min(n0 + 16 * t + r, N - 1)) * (BY_TOKEN ? B.ld : 1) * SIZE;
     if (BT == SPMM_I8 && threadIdx.x < 16 * NT) token_scales[threadIdx.x] = B_scales[min(n0 + (int64_t)threadIdx.x, N - 1)];
+    // STAGED, for one tile of tokens, one a row of memory: a load of operands touches all 16 rows for 8 to 32 bytes each, and the vector L1 takes 3 clocks a row.  So
+    // lanes read along the rows instead, 16 bytes each, and operands change places in LDS.  (Rows that do not exist are read as the last one and cost nothing.)
+    static_assert(!STAGED || (BY_TOKEN && NT == 1 && !FMA));
+    constexpr int ROW_LANES = 8 * (int)SIZE, ROWS_AT_ONCE = 64 / ROW_LANES, PIECES = 16 / ROWS_AT_ONCE, PART_SIZE = BT == SPMM_I8 ? 1 : 2, PITCH = BLOCK_COLS * PART_SIZE + 16;
+    __shared__ __align__(16) char staged[STAGED ? KWAVES * PARTS<BT> * 16 * PITCH : 16];
     struct asked {
         u32x4 word[RT];
         span_values<SUMS, ZEROS> span[RT];
-        raw<BT> b[NT][4];
+        raw<BT> b[NT][4];       // operands as they are read
+        u32x4 piece[PIECES];    // STAGED: pieces of rows
     };
     auto ask = [&](int b, asked &a, auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
+        if constexpr (STAGED && !TAIL) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                const int row = min(p * ROWS_AT_ONCE + lane / ROW_LANES, (int)N - 1);
+                a.piece[p] = __builtin_bit_cast(u32x4, *reinterpret_cast<const neighbours<typename stored<BT>::type, 16 / SIZE> *>(B.data + row * B.ld * SIZE + (int64_t)b * (BLOCK_COLS * SIZE) + lane % ROW_LANES * 16));
+            }
+        }
 #pragma unroll
         for (int i = 0; i < RT; ++i) a.word[i] = reinterpret_cast<const u32x4 *>(codes + ((int64_t)i * W.blocks + b) * BLOCK_WORDS)[lane];
         const int left = (int)(W.K - (int64_t)b * BLOCK_COLS);
+        if constexpr (!STAGED || TAIL)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -605,7 +619,42 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
-    auto use = [&](const asked &a) {
+    auto use = [&](const asked &a, auto tail) {
+        operands<BT> o[NT][4];
+        if constexpr (STAGED && !decltype(tail)::value) {
+            char *const mine = staged + wave * (PARTS<BT> * 16 * PITCH);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                char *const to = mine + (p * ROWS_AT_ONCE + lane / ROW_LANES) * PITCH + lane % ROW_LANES * (16 / SIZE * PART_SIZE);
+                if constexpr (BT == SPMM_F32) {
+                    raw<BT> x = {};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t bits = a.piece[p][j];  // (a bit cast of a vector's element itself is one of its first)
+                        x.v[j] = __builtin_bit_cast(float, bits);
+                    }
+                    const operands<BT> parts = operands_of<BT>(x);
+#pragma unroll
+                    for (int part = 0; part < 3; ++part) *reinterpret_cast<u32x2 *>(to + part * 16 * PITCH) = u32x2{parts.part[part][0], parts.part[part][1]};
+                } else {
+                    *reinterpret_cast<u32x4 *>(to) = a.piece[p];
+                }
+            }
+            const char *const from = mine + r * PITCH + 8 * q * PART_SIZE;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if constexpr (BT == SPMM_I8) {
+                    o[0][s] = operands_of<BT>(raw<BT>{*reinterpret_cast<const u32x2 *>(from + 32 * s)});
+                } else {
+#pragma unroll
+                    for (int part = 0; part < PARTS<BT>; ++part) o[0][s].part[part] = *reinterpret_cast<const u32x4 *>(from + part * 16 * PITCH + 64 * s);
+                }
+            }
+        }
+        auto operand = [&](int t, int s) {
+            if constexpr (STAGED && !decltype(tail)::value) return o[t][s];
+            else return operands_of<BT>(a.b[t][s]);
+        };
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             // (one tile's weights at a time: the registers do not hold all of them as operands)
@@ -643,12 +692,12 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
                     i32x4 part;
 #pragma unroll
                     for (int s = 0; s < 4; s += PER_GROUP == 1 ? 1 : 2) {
-                        const u32x2 x0 = operands_of<BT>(a.b[t][s]).part[0];
+                        const u32x2 x0 = operand(t, s).part[0];
                         if constexpr (PER_GROUP == 1) {
                             const int h = 2 * (s % 2);
                             part = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, x0), (long)((uint64_t)w[s / 2][h] | (uint64_t)w[s / 2][h + 1] << 32), i32x4{0, 0, 0, 0}, 0, 0, 0);
                         } else {
-                            const u32x2 x1 = operands_of<BT>(a.b[t][s + 1]).part[0];
+                            const u32x2 x1 = operand(t, s + 1).part[0];
                             const i32x4 x = {(int)x0[0], (int)x0[1], (int)x1[0], (int)x1[1]};
                             part = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, __builtin_bit_cast(i32x4, w[s / 2]), s % PER_GROUP == 0 ? i32x4{0, 0, 0, 0} : part, 0, 0, 0);
                         }
@@ -661,12 +710,12 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
                     f32x4 part;
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
-                        const operands<BT> o = operands_of<BT>(a.b[t][s]);
+                        const operands<BT> x = operand(t, s);
                         if (s % PER_GROUP == 0) part = f32x4{0, 0, 0, 0};
 #pragma unroll
                         for (int p = PARTS<BT> - 1; p >= 0; --p) {
-                            if constexpr (BT == SPMM_F16) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, o.part[p]), __builtin_bit_cast(f16x8, w[s]), part, 0, 0, 0);
-                            else part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o.part[p]), __builtin_bit_cast(bf16x8, w[s]), part, 0, 0, 0);
+                            if constexpr (BT == SPMM_F16) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x.part[p]), __builtin_bit_cast(f16x8, w[s]), part, 0, 0, 0);
+                            else part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.part[p]), __builtin_bit_cast(bf16x8, w[s]), part, 0, 0, 0);
                         }
                         if (s % PER_GROUP == PER_GROUP - 1) {
 #pragma unroll
@@ -687,13 +736,13 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             if (b + i >= whole) break;
-            use(ring[i]);
+            use(ring[i], std::false_type());
             if (b + i + AHEAD < whole) ask(b + i + AHEAD, ring[i], std::false_type());
         }
     }
     if (whole < last) {
         ask(whole, ring[0], std::true_type());
-        use(ring[0]);
+        use(ring[0], std::true_type());
     }
     if constexpr (FMA) {  // the four quarters of the columns
 #pragma unroll
@@ -724,27 +773,38 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
 // Token by token of fp32 by multiply-adds, else on the matrix cores.  Tiles: a wave has more where workgroups are left over otherwise (256 compute units).
 template <int BT, bool BY_TOKEN, bool FMA> hipError_t execute_direct(const quant_matrix &w, const tensor &B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
-    auto shaped = [&](auto per_group, auto rt, auto nt, auto kwaves, auto ahead) {
+    auto shaped = [&](auto per_group, auto rt, auto nt, auto kwaves, auto ahead, auto staged) {
         constexpr int PER_GROUP = decltype(per_group)::value, RT = decltype(rt)::value, NT = decltype(nt)::value, KWAVES = decltype(kwaves)::value, AHEAD = decltype(ahead)::value;
+        constexpr bool STAGED = decltype(staged)::value;
         const dim3 blocks((unsigned)((w.tiles + RT - 1) / RT), (unsigned)((N + 16 * NT - 1) / (16 * NT)));
-        if (w.zeros) return launch_kernel(direct_kernel<BT, BY_TOKEN, PER_GROUP, RT, NT, KWAVES, AHEAD, FMA, true>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, N, C);
-        return launch_kernel(direct_kernel<BT, BY_TOKEN, PER_GROUP, RT, NT, KWAVES, AHEAD, FMA, false>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, N, C);
+        if (w.zeros) return launch_kernel(direct_kernel<BT, BY_TOKEN, PER_GROUP, RT, NT, KWAVES, AHEAD, FMA, STAGED, true>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, N, C);
+        return launch_kernel(direct_kernel<BT, BY_TOKEN, PER_GROUP, RT, NT, KWAVES, AHEAD, FMA, STAGED, false>, blocks, 64 * KWAVES, 0, stream, w, B, B_scales, N, C);
     };
     auto run = [&](auto per_group) {
         constexpr int PER_GROUP = decltype(per_group)::value;
+        constexpr std::false_type no = {};
         if constexpr (!FMA) {
-            if (N > 16) {
-                return shaped(per_group, constant<1>(), constant<2>(), constant<8>(), constant<1>());
-            }
+            if (N > 16) return shaped(per_group, constant<1>(), constant<2>(), constant<8>(), constant<1>(), no);
         }
         // (what the registers hold)
         constexpr int AHEAD = BT == SPMM_F32 && !FMA ? 1 : 2, LESS = PER_GROUP < 4 || FMA ? 1 : AHEAD;
         constexpr int MOST = PER_GROUP == 1 || (BT == SPMM_F32 && !BY_TOKEN) ? 2 : 4;
-        if (w.tiles >= 1024) return shaped(per_group, constant<MOST>(), constant<1>(), constant<8>(), constant<LESS>());
-        if (w.tiles >= 512) return shaped(per_group, constant<2>(), constant<1>(), constant<8>(), constant<AHEAD>());
-        if constexpr (BY_TOKEN && BT != SPMM_F32)
-            if (w.blocks > 8) return shaped(per_group, constant<1>(), constant<1>(), constant<16>(), constant<LESS>());
-        return shaped(per_group, constant<1>(), constant<1>(), constant<8>(), constant<1>());
+        // STAGED or straight, us.  1024 x 4096: one token in codes 3.4 and 3.6, 16 3.6 and 6.2; in bf16 one 4.1 and 3.6, 4 4.1 and 4.2, 16 4.4 and 6.2.  8192 x 8192, two tiles of rows: 16 in codes
+        // 10.3 and 12.3, in bf16 8 11.7 and 11.1, 16 12.3 and 13.0.  With four tiles a wave B is read less often: 16384 x 16384, one in codes 37.7 and 34.3, 16 34.8 and 34.9.  fp32, whose parts
+        // are made once then: 3 on 1024 x 4096 8.8 and 7.7, on 8192 x 8192 21.5 and 24.7, on 16384 x 16384 54 and 90.  256 x 256, where all is one wait: 2.5 and 2.4, fp32 3.8 and 3.3.
+        constexpr std::bool_constant<BY_TOKEN && !FMA> yes = {};
+        constexpr std::bool_constant<yes() && BT == SPMM_F32> parts = {};
+        constexpr bool SPLIT = BY_TOKEN && BT != SPMM_F32, HALF = SPLIT && BT != SPMM_I8;
+        if (w.tiles >= 1024) return shaped(per_group, constant<MOST>(), constant<1>(), constant<8>(), constant<LESS>(), parts);
+        if constexpr (HALF) {
+            if (w.tiles >= 512 && N <= 8) return shaped(per_group, constant<2>(), constant<1>(), constant<8>(), constant<AHEAD>(), no);
+            if (w.tiles < 512 && w.blocks > 8 && N <= 4) return shaped(per_group, constant<1>(), constant<1>(), constant<16>(), constant<LESS>(), no);
+        }
+        if (w.tiles >= 512) return shaped(per_group, constant<2>(), constant<1>(), constant<8>(), constant<AHEAD>(), yes);
+        if constexpr (SPLIT) {
+            if (w.blocks > 8) return shaped(per_group, constant<1>(), constant<1>(), constant<16>(), constant<LESS>(), yes);
+        }
+        return shaped(per_group, constant<1>(), constant<1>(), constant<8>(), constant<1>(), no);
     };
     if (w.group == 32) return run(constant<1>());
     if (w.group == 64) return run(constant<2>());
