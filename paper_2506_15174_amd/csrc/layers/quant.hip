@@ -403,27 +403,27 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 
 // ---- prompts -----------------------------------------------------------------------------------------------------
 //
-// A wave has 64 rows and 64 tokens (32 in fp32, whose three parts take the registers).  Of a workgroup's eight, ROW_WAVES lie one below the other and share their tokens' B, TOKEN_WAVES side by side, and K_WAVES
-// such groups share K; their sums meet in LDS at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock (1 KiB feeds four
-// instructions of 16 clocks on each of four SIMDs); it is on its way there by stages of STAGE steps of 32 columns while the stage before is multiplied.  Weights are made operands by
-// each wave for itself: 52 instructions a step beside 16 of the matrix unit, two waves to a SIMD, is about what keeps both busy.
+// A workgroup has 128 rows and 64 tokens.  Its eight waves have 64 rows and all of the tokens each: two lie one below the other and share the tokens' B, and K is split over four such
+// pairs, whose sums meet in LDS at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock (1 KiB feeds four
+// instructions of 16 clocks on each of four SIMDs); a block of 128 columns is on its way there while the block before is multiplied.  Weights are made operands by
+// each wave for itself: 52 instructions for 32 columns beside 16 of the matrix unit, two waves to a SIMD, is about what keeps both busy.
+// 8192 x 8192, 512 tokens in bf16: 99 us, 694 TF, and 6 to lay out B.  The products alone take 67, the loads alone 60.
 
-template <int BT> constexpr int WIDE_NT = BT == SPMM_F32 ? 2 : 4;
+constexpr int WIDE_TILES = 4, WIDE_PAIRS = 4, WIDE_STAGE = WIDE_TILES * 4096, WIDE_LDS = 2 * WIDE_PAIRS * WIDE_STAGE;
 
-template <int BT, int ROW_WAVES, int TOKEN_WAVES, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N, tensor C)
+template <int BT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, int64_t N, tensor C)
 {
+    static_assert(BT == SPMM_F16 || BT == SPMM_BF16);
     extern __shared__ __align__(16) char lds[];
-    constexpr int RT = 4, NT = WIDE_NT<BT>, K_WAVES = 8 / (ROW_WAVES * TOKEN_WAVES), TILES = NT * TOKEN_WAVES, SUMS = 4 / STEPS, P = PARTS<BT>, BLOCK_BYTES = 4 * P * STEP_BYTES<BT>;
-    constexpr int STAGE = BT == SPMM_F32 ? 1 : 4, STAGES = 4 / STAGE, TILE_BYTES = BLOCK_BYTES / STAGES, STAGE_BYTES = TILES * TILE_BYTES;
-    constexpr int LOADS = TILE_BYTES / 1024, EACH = TILES * LOADS / ROW_WAVES / TOKEN_WAVES;
-    static_assert(EACH * ROW_WAVES * TOKEN_WAVES == TILES * LOADS);
+    constexpr int RT = WIDE_TILES, NT = WIDE_TILES, SUMS = 4 / STEPS, BLOCK_BYTES = 4 * STEP_BYTES<BT>, EACH = WIDE_STAGE / 1024 / 2;
+    static_assert(BLOCK_BYTES * NT == WIDE_STAGE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
-    const int row_wave = wave % ROW_WAVES, token_wave = wave / ROW_WAVES % TOKEN_WAVES, k_wave = wave / (ROW_WAVES * TOKEN_WAVES), sharer = wave % (ROW_WAVES * TOKEN_WAVES);
-    const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * TILES, wg_tile0 = (int64_t)blockIdx.x * (RT * ROW_WAVES);
+    const int half = wave & 1, pair = wave >> 1;
+    const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * NT, wg_tile0 = (int64_t)blockIdx.x * (2 * RT);
     // (a wave whose rows do not exist has the last ones)
-    const int64_t tile0 = min(wg_tile0 + row_wave * RT, ((int64_t)W.tiles - 1) / RT * RT);
-    const int first = (int)((int64_t)W.blocks * k_wave / K_WAVES), last = (int)((int64_t)W.blocks * (k_wave + 1) / K_WAVES);
-    const int rounds = (W.blocks + K_WAVES - 1) / K_WAVES;  // as many for every wave, for the barriers
+    const int64_t tile0 = min(wg_tile0 + half * RT, ((int64_t)W.tiles - 1) / RT * RT);
+    const int first = (int)((int64_t)W.blocks * pair / WIDE_PAIRS), last = (int)((int64_t)W.blocks * (pair + 1) / WIDE_PAIRS);
+    const int rounds = (W.blocks + WIDE_PAIRS - 1) / WIDE_PAIRS;  // as many for every wave, for the barriers
     const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
     struct asked {
         u32x4 word[RT];
@@ -436,120 +436,86 @@ template <int BT, int ROW_WAVES, int TOKEN_WAVES, int STEPS, bool ZEROS> __globa
             a.span[i] = span_of<SUMS, ZEROS>(W, tile0 + i, b, r);
         }
     };
-    // This wave's share of a stage of B, straight to LDS: [place][k_wave][tile of tokens][1 KiB each]
-    auto place_of = [&](int place) { return lds + (place * K_WAVES + k_wave) * STAGE_BYTES; };
-    auto send = [&](int b, int stage, int place) {
+    // This wave's share of a block of B, straight to LDS: [place][pair][tile of tokens][4 KiB each]
+    auto place_of = [&](int place) { return lds + (place * WIDE_PAIRS + pair) * WIDE_STAGE; };
+    auto send = [&](int b, int place) {
 #pragma unroll
         for (int l = 0; l < EACH; ++l) {
-            const int at = sharer * EACH + l;
-            const char *from = B + (min(token0 + at / LOADS, token_tiles - 1) * W.blocks + b) * BLOCK_BYTES + stage * TILE_BYTES + at % LOADS * 1024 + lane * 16;
+            const int at = half * EACH + l;
+            const char *from = B + (min(token0 + at / 4, token_tiles - 1) * W.blocks + b) * BLOCK_BYTES + at % 4 * 1024 + lane * 16;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)(place_of(place) + at * 1024), 16, 0, 0);
         }
     };
-    typedef std::conditional_t<BT == SPMM_I8, i32x4, f32x4> sum;
-    f32x4 acc[RT][NT];
-    sum part[RT][NT];
+    f32x4 acc[RT][NT], part[RT][NT];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
     asked now, next;
     if (first < last) {
-        send(first, 0, 0);
+        send(first, 0);
         ask(first, now);
     }
     for (int round = 0; round < rounds; ++round) {
         const int b = first + round;
+        // This wave's share of the block is there (and what it asked for besides), then the other's; both have read the block before.
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (b >= last) continue;
+        if (b + 1 < last) {
+            send(b + 1, (round + 1) & 1);
+            ask(b + 1, next);
+        }
+        const char *const from = place_of(round & 1) + lane * 16;
 #pragma unroll
-        for (int stage = 0; stage < STAGES; ++stage) {
-            const int place = STAGES > 1 ? stage & 1 : round & 1;
-            // This wave's share of the stage is there (and what it asked for besides), then the others'; all have read the stage before.
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (b >= last) continue;
-            if (stage + 1 < STAGES) send(b, stage + 1, place ^ 1);
-            else if (b + 1 < last) send(b + 1, 0, place ^ 1);
-            if (stage == STAGES - 1 && b + 1 < last) ask(b + 1, next);
-            const char *const from = place_of(place) + token_wave * (NT * TILE_BYTES) + lane * 16;
+        for (int s = 0; s < 4; ++s) {
+            if (STEPS < 4) __builtin_amdgcn_sched_barrier(0);  // (scales of several groups: no registers for two steps at a time)
+            u32x4 w[RT], x[NT];
 #pragma unroll
-            for (int h = 0; h < STAGE; h += BT == SPMM_I8 && STEPS > 1 ? 2 : 1) {
-                const int s = stage * STAGE + h;
-                const bool begins = s % STEPS == 0;
-                if (STEPS < 4) __builtin_amdgcn_sched_barrier(0);  // (scales of several groups: no registers for two steps at a time)
-                if constexpr (BT == SPMM_I8) {
-                    i32x4 x[NT];
+            for (int i = 0; i < RT; ++i) {
+                if constexpr (BT == SPMM_F16) w[i] = __builtin_bit_cast(u32x4, weights_f16(now.word[i][s], now.span[i].zero(s / STEPS)));
+                else w[i] = __builtin_bit_cast(u32x4, weights_bf16<ZEROS>(now.word[i][s], now.span[i].zero(s / STEPS)));
+            }
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const i32x4 *>(from + t * TILE_BYTES + h / 2 * 1024);
+            for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const u32x4 *>(from + t * BLOCK_BYTES + s * 1024);
 #pragma unroll
-                    for (int i = 0; i < RT; ++i) {
-                        const u32x2 w0 = weights_i8(now.word[i][s], (uint32_t)now.span[i].zero(s / STEPS) * 0x01010101u);
-                        if constexpr (STEPS == 1) {
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-                            for (int t = 0; t < NT; ++t)
-                                part[i][t] = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)((uint64_t)(uint32_t)x[t][2 * (h % 2)] | (uint64_t)(uint32_t)x[t][2 * (h % 2) + 1] << 32),
-                                                                                   __builtin_bit_cast(long, w0), sum{0, 0, 0, 0}, 0, 0, 0);
-                        } else {
-                            const u32x2 w1 = weights_i8(now.word[i][s + 1], (uint32_t)now.span[i].zero(s / STEPS) * 0x01010101u);
-                            const i32x4 w = {(int)w0[0], (int)w0[1], (int)w1[0], (int)w1[1]};
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) part[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w, begins ? sum{0, 0, 0, 0} : part[i][t], 0, 0, 0);
-                        }
-                    }
-                } else {
-                    u32x4 w[RT];
-#pragma unroll
-                    for (int i = 0; i < RT; ++i) {
-                        if constexpr (BT == SPMM_F16) w[i] = __builtin_bit_cast(u32x4, weights_f16(now.word[i][s], now.span[i].zero(s / STEPS)));
-                        else w[i] = __builtin_bit_cast(u32x4, weights_bf16<ZEROS>(now.word[i][s], now.span[i].zero(s / STEPS)));
-                    }
-#pragma unroll
-                    for (int p = P - 1; p >= 0; --p) {
-                        u32x4 x[NT];
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const u32x4 *>(from + t * TILE_BYTES + (h * P + p) * 1024);
-#pragma unroll
-                        for (int i = 0; i < RT; ++i)
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                sum &to = part[i][t];
-                                const sum c = begins && p == P - 1 ? sum{0, 0, 0, 0} : to;
-                                if constexpr (BT == SPMM_F16) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[t]), __builtin_bit_cast(f16x8, w[i]), c, 0, 0, 0);
-                                else to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, w[i]), c, 0, 0, 0);
-                            }
-                    }
+                for (int t = 0; t < NT; ++t) {
+                    const f32x4 c = s % STEPS == 0 ? f32x4{0, 0, 0, 0} : part[i][t];
+                    if constexpr (BT == SPMM_F16) part[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[t]), __builtin_bit_cast(f16x8, w[i]), c, 0, 0, 0);
+                    else part[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, w[i]), c, 0, 0, 0);
                 }
-                if (s % STEPS == STEPS - 1 || (BT == SPMM_I8 && (s + 1) % STEPS == STEPS - 1)) {
+            if (s % STEPS == STEPS - 1) {
 #pragma unroll
-                    for (int i = 0; i < RT; ++i)
+                for (int i = 0; i < RT; ++i)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][t][e] += now.span[i].scale[s / STEPS] * WEIGHT_UNIT<BT> * (float)part[i][t][e];
-                }
+                        for (int e = 0; e < 4; ++e) acc[i][t][e] += now.span[i].scale[s / STEPS] * WEIGHT_UNIT<BT> * part[i][t][e];
             }
         }
         now = next;
     }
-    // The sums of the groups that share K meet in LDS: [k_wave][tile of rows][tile of tokens][256]
+    // The pairs' sums meet in LDS: [pair][tile of rows][tile of tokens][256]
     __syncthreads();
     float *const sums = reinterpret_cast<float *>(lds);
-    constexpr int ROW_TILES = RT * ROW_WAVES;
+    constexpr int ROW_TILES = 2 * RT;
+    static_assert(WIDE_PAIRS * ROW_TILES * NT * 1024 <= WIDE_LDS);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-            *reinterpret_cast<f32x4 *>(sums + ((k_wave * ROW_TILES + row_wave * RT + i) * TILES + token_wave * NT + t) * 256 + lane * 4) = acc[i][t];
+        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(sums + ((pair * ROW_TILES + half * RT + i) * NT + t) * 256 + lane * 4) = acc[i][t];
     __syncthreads();
-    for (int e = threadIdx.x; e < ROW_TILES * TILES * 256; e += 512) {
-        const int m = C.by_token ? e % (16 * ROW_TILES) : e / (16 * TILES), t = C.by_token ? e / (16 * ROW_TILES) : e % (16 * TILES);
+    for (int e = threadIdx.x; e < ROW_TILES * NT * 256; e += 512) {
+        const int m = C.by_token ? e % (16 * ROW_TILES) : e / (16 * NT), t = C.by_token ? e / (16 * ROW_TILES) : e % (16 * NT);
         const int64_t row = wg_tile0 * TILE_ROWS + m, n = token0 * 16 + t;
         if (row >= W.M || n >= N) continue;
-        const int at = ((m / 16) * TILES + t / 16) * 256 + ((t & 15) >> 2) * 64 + (m % 16) * 4 + (t & 3);
+        const int at = ((m / 16) * NT + t / 16) * 256 + ((t & 15) >> 2) * 64 + (m % 16) * 4 + (t & 3);
         float v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < K_WAVES; ++k) v += sums[k * ROW_TILES * TILES * 256 + at];
-        if (BT == SPMM_I8) v *= B_scales[n];
+        for (int k = 0; k < WIDE_PAIRS; ++k) v += sums[k * ROW_TILES * NT * 256 + at];
         store_as(C.data, C.by_token ? n * C.ld + row : row * C.ld + n, C.type, v);
     }
 }
@@ -826,16 +792,14 @@ template <int BT, int NT, int RT, int KWAVES> hipError_t launch_many(const quant
     return run(constant<4>());
 }
 
-template <int BT, int ROW_WAVES, int TOKEN_WAVES> hipError_t launch_wide(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
+template <int BT> hipError_t launch_wide(const quant_matrix &w, const char *B, int64_t N, const tensor &C, hipStream_t stream)
 {
-    constexpr int ROWS = 4 * ROW_WAVES, TILES = WIDE_NT<BT> * TOKEN_WAVES, K_WAVES = 8 / (ROW_WAVES * TOKEN_WAVES);
-    constexpr unsigned STAGES = 2 * K_WAVES * TILES * PARTS<BT> * STEP_BYTES<BT> * (BT == SPMM_F32 ? 1 : 4), SUMS = 8 * 4 * WIDE_NT<BT> * 1024, LDS = STAGES > SUMS ? STAGES : SUMS;
-    static_assert(LDS <= 160 * 1024);
-    const dim3 blocks((unsigned)((w.tiles + ROWS - 1) / ROWS), (unsigned)((N + 16 * TILES - 1) / (16 * TILES)));
-    auto shaped = [&](auto per_group, auto zeros) {
-        return launch_kernel(wide_kernel<BT, ROW_WAVES, TOKEN_WAVES, decltype(per_group)::value, decltype(zeros)::value>, blocks, 512, LDS, stream, w, B, B_scales, N, C);
+    const dim3 blocks((unsigned)((w.tiles + 2 * WIDE_TILES - 1) / (2 * WIDE_TILES)), (unsigned)((N + 16 * WIDE_TILES - 1) / (16 * WIDE_TILES)));
+    auto run = [&](auto per_group) {
+        constexpr int PER_GROUP = decltype(per_group)::value;
+        if (w.zeros) return launch_kernel(wide_kernel<BT, PER_GROUP, true>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
+        return launch_kernel(wide_kernel<BT, PER_GROUP, false>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
     };
-    auto run = [&](auto per_group) { return w.zeros ? shaped(per_group, std::true_type()) : shaped(per_group, std::false_type()); };
     if (w.group == 32) return run(constant<1>());
     if (w.group == 64) return run(constant<2>());
     return run(constant<4>());
@@ -859,7 +823,7 @@ template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, 
         if (workgroups(4, 4) >= 480) return launch_many<BT, 4, 4, 4>(w, B, B_scales, N, C, stream);
     } else {
         const int64_t wide = workgroups(8, 4), rounds = (wide + 255) / 256;
-        if (w.K >= 4096 && wide * 10 >= rounds * 256 * 9) return launch_wide<BT, 2, 1>(w, B, B_scales, N, C, stream);
+        if (w.K >= 4096 && wide * 10 >= rounds * 256 * 9) return launch_wide<BT>(w, B, N, C, stream);
     }
     return launch_many<BT, 2, 2, 8>(w, B, B_scales, N, C, stream);
 }
