@@ -8,6 +8,7 @@
 // needs one scale a group.
 //
 // pack_kernel lays B out as the instructions take it; product_kernel gives a tile of 16 rows and up to 128 tokens to a workgroup, whose waves share K.
+#include <algorithm>
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -403,27 +404,29 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 
 // ---- prompts -----------------------------------------------------------------------------------------------------
 //
-// A workgroup has 128 rows and 64 tokens.  Its eight waves have 64 rows and all of the tokens each: two lie one below the other and share the tokens' B, and K is split over four such
-// pairs, whose sums meet in LDS at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock (1 KiB feeds four
-// instructions of 16 clocks on each of four SIMDs); a block of 128 columns is on its way there while the block before is multiplied.  Weights are made operands by
-// each wave for itself: 52 instructions for 32 columns beside 16 of the matrix unit, two waves to a SIMD, is about what keeps both busy.
-// 8192 x 8192, 512 tokens in bf16: 99 us, 694 TF, and 6 to lay out B.  The products alone take 67, the loads alone 60.
+// A wave has 64 rows and 64 tokens.  Of a workgroup's eight, teams of SHARE lie one below the other and share the tokens' B; K is split over the 8 / SHARE teams, whose sums meet in LDS
+// at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock (1 KiB feeds four instructions of 16 clocks on each of four SIMDs); a
+// block of 128 columns is on its way there while the block before is multiplied.  A team waits for its own waves only: with a barrier for the workgroup 8192 x 8192, 512 tokens, took
+// 105 us, without 89 (teams of two).  Weights are made operands by each wave for itself: 52 instructions for 32 columns beside 16 of the matrix unit, two waves to a SIMD, is about what
+// keeps both busy.  In bf16, with 6 us to lay out B for 512 tokens: 83 us, 825 TF; 4096 tokens 586, 938 TF.
 
-constexpr int WIDE_TILES = 4, WIDE_PAIRS = 4, WIDE_STAGE = WIDE_TILES * 4096, WIDE_LDS = 2 * WIDE_PAIRS * WIDE_STAGE;
+constexpr int WIDE_TILES = 4, WIDE_STAGE = WIDE_TILES * 4096, WIDE_LDS = 8 * WIDE_TILES * WIDE_TILES * 1024;
 
-template <int BT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, int64_t N, tensor C)
+template <int BT, int SHARE, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, int64_t N, tensor C)
 {
     static_assert(BT == SPMM_F16 || BT == SPMM_BF16);
     extern __shared__ __align__(16) char lds[];
-    constexpr int RT = WIDE_TILES, NT = WIDE_TILES, SUMS = 4 / STEPS, BLOCK_BYTES = 4 * STEP_BYTES<BT>, EACH = WIDE_STAGE / 1024 / 2;
-    static_assert(BLOCK_BYTES * NT == WIDE_STAGE);
+    constexpr int TEAMS = 8 / SHARE, RT = WIDE_TILES, NT = WIDE_TILES, SUMS = 4 / STEPS, BLOCK_BYTES = 4 * STEP_BYTES<BT>, EACH = WIDE_STAGE / 1024 / SHARE;
+    static_assert(BLOCK_BYTES * NT == WIDE_STAGE && 2 * TEAMS * WIDE_STAGE <= WIDE_LDS);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
-    const int half = wave & 1, pair = wave >> 1;
-    const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * NT, wg_tile0 = (int64_t)blockIdx.x * (2 * RT);
+    const int member = wave % SHARE, team = wave / SHARE;
+    const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * NT, wg_tile0 = (int64_t)blockIdx.x * (SHARE * RT);
     // (a wave whose rows do not exist has the last ones)
-    const int64_t tile0 = min(wg_tile0 + half * RT, ((int64_t)W.tiles - 1) / RT * RT);
-    const int first = (int)((int64_t)W.blocks * pair / WIDE_PAIRS), last = (int)((int64_t)W.blocks * (pair + 1) / WIDE_PAIRS);
-    const int rounds = (W.blocks + WIDE_PAIRS - 1) / WIDE_PAIRS;  // as many for every wave, for the barriers
+    const int64_t tile0 = min(wg_tile0 + member * RT, ((int64_t)W.tiles - 1) / RT * RT);
+    const int first = (int)((int64_t)W.blocks * team / TEAMS), last = (int)((int64_t)W.blocks * (team + 1) / TEAMS);
+    __shared__ int arrived[8];  // blocks whose share of B a wave has brought
+    if (threadIdx.x < 8) arrived[threadIdx.x] = 0;
+    __syncthreads();
     const uint32_t *const codes = W.codes + tile0 * W.blocks * BLOCK_WORDS;
     struct asked {
         u32x4 word[RT];
@@ -436,12 +439,12 @@ template <int BT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void 
             a.span[i] = span_of<SUMS, ZEROS>(W, tile0 + i, b, r);
         }
     };
-    // This wave's share of a block of B, straight to LDS: [place][pair][tile of tokens][4 KiB each]
-    auto place_of = [&](int place) { return lds + (place * WIDE_PAIRS + pair) * WIDE_STAGE; };
+    // This wave's share of a block of B, straight to LDS: [place][team][tile of tokens][4 KiB each]
+    auto place_of = [&](int place) { return lds + (place * TEAMS + team) * WIDE_STAGE; };
     auto send = [&](int b, int place) {
 #pragma unroll
         for (int l = 0; l < EACH; ++l) {
-            const int at = half * EACH + l;
+            const int at = member * EACH + l;
             const char *from = B + (min(token0 + at / 4, token_tiles - 1) * W.blocks + b) * BLOCK_BYTES + at % 4 * 1024 + lane * 16;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)(place_of(place) + at * 1024), 16, 0, 0);
         }
@@ -456,17 +459,15 @@ template <int BT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void 
         send(first, 0);
         ask(first, now);
     }
-    for (int round = 0; round < rounds; ++round) {
-        const int b = first + round;
-        // This wave's share of the block is there (and what it asked for besides), then the other's; both have read the block before.
+    for (int b = first; b < last; ++b) {
+        const int round = b - first;
+        // This wave's share of the block is there (and what it asked for besides), then the team's; all of them have read the block before.
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
+        __hip_atomic_store(&arrived[wave], round + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        if (b + 1 < last) ask(b + 1, next);
+        while (!__all(__hip_atomic_load(&arrived[team * SHARE + lane % SHARE], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > round)) {}
         asm volatile("" ::: "memory");
-        if (b >= last) continue;
-        if (b + 1 < last) {
-            send(b + 1, (round + 1) & 1);
-            ask(b + 1, next);
-        }
+        if (b + 1 < last) send(b + 1, (round + 1) & 1);
         const char *const from = place_of(round & 1) + lane * 16;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -498,15 +499,15 @@ template <int BT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void 
         }
         now = next;
     }
-    // The pairs' sums meet in LDS: [pair][tile of rows][tile of tokens][256]
+    // The teams' sums meet in LDS: [team][tile of rows][tile of tokens][256]
     __syncthreads();
     float *const sums = reinterpret_cast<float *>(lds);
-    constexpr int ROW_TILES = 2 * RT;
-    static_assert(WIDE_PAIRS * ROW_TILES * NT * 1024 <= WIDE_LDS);
+    constexpr int ROW_TILES = SHARE * RT;
+    static_assert(TEAMS * ROW_TILES * NT * 1024 == WIDE_LDS);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(sums + ((pair * ROW_TILES + half * RT + i) * NT + t) * 256 + lane * 4) = acc[i][t];
+        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(sums + ((team * ROW_TILES + member * RT + i) * NT + t) * 256 + lane * 4) = acc[i][t];
     __syncthreads();
     for (int e = threadIdx.x; e < ROW_TILES * NT * 256; e += 512) {
         const int m = C.by_token ? e % (16 * ROW_TILES) : e / (16 * NT), t = C.by_token ? e / (16 * ROW_TILES) : e % (16 * NT);
@@ -515,7 +516,7 @@ template <int BT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void 
         const int at = ((m / 16) * NT + t / 16) * 256 + ((t & 15) >> 2) * 64 + (m % 16) * 4 + (t & 3);
         float v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < WIDE_PAIRS; ++k) v += sums[k * ROW_TILES * NT * 256 + at];
+        for (int k = 0; k < TEAMS; ++k) v += sums[k * ROW_TILES * NT * 256 + at];
         store_as(C.data, C.by_token ? n * C.ld + row : row * C.ld + n, C.type, v);
     }
 }
@@ -792,13 +793,13 @@ template <int BT, int NT, int RT, int KWAVES> hipError_t launch_many(const quant
     return run(constant<4>());
 }
 
-template <int BT> hipError_t launch_wide(const quant_matrix &w, const char *B, int64_t N, const tensor &C, hipStream_t stream)
+template <int BT, int SHARE> hipError_t launch_wide(const quant_matrix &w, const char *B, int64_t N, const tensor &C, hipStream_t stream)
 {
-    const dim3 blocks((unsigned)((w.tiles + 2 * WIDE_TILES - 1) / (2 * WIDE_TILES)), (unsigned)((N + 16 * WIDE_TILES - 1) / (16 * WIDE_TILES)));
+    const dim3 blocks((unsigned)((w.tiles + SHARE * WIDE_TILES - 1) / (SHARE * WIDE_TILES)), (unsigned)((N + 16 * WIDE_TILES - 1) / (16 * WIDE_TILES)));
     auto run = [&](auto per_group) {
         constexpr int PER_GROUP = decltype(per_group)::value;
-        if (w.zeros) return launch_kernel(wide_kernel<BT, PER_GROUP, true>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
-        return launch_kernel(wide_kernel<BT, PER_GROUP, false>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
+        if (w.zeros) return launch_kernel(wide_kernel<BT, SHARE, PER_GROUP, true>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
+        return launch_kernel(wide_kernel<BT, SHARE, PER_GROUP, false>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
     };
     if (w.group == 32) return run(constant<1>());
     if (w.group == 64) return run(constant<2>());
@@ -822,8 +823,14 @@ template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, 
     } else if constexpr (BT == SPMM_I8) {
         if (workgroups(4, 4) >= 480) return launch_many<BT, 4, 4, 4>(w, B, B_scales, N, C, stream);
     } else {
-        const int64_t wide = workgroups(8, 4), rounds = (wide + 255) / 256;
-        if (w.K >= 4096 && wide * 10 >= rounds * 256 * 9) return launch_wide<BT>(w, B, N, C, stream);
+        // Rounds of 256 workgroups, by what one takes (of 8192 columns 8, 41, 76 and 137 us): the fewer rows a team has, the more often B is read.
+        auto us = [&](int64_t rows, int64_t tokens, int64_t round) { return (workgroups(rows, tokens) + 255) / 256 * round; };
+        const int64_t two = us(8, 4, 41), four = us(16, 4, 76), eight = us(32, 4, 137);
+        if (std::min({two, four, eight}) < us(2, 2, 8)) {
+            if (eight <= std::min(two, four)) return launch_wide<BT, 8>(w, B, N, C, stream);
+            if (four <= two) return launch_wide<BT, 4>(w, B, N, C, stream);
+            return launch_wide<BT, 2>(w, B, N, C, stream);
+        }
     }
     return launch_many<BT, 2, 2, 8>(w, B, B_scales, N, C, stream);
 }
