@@ -1,7 +1,7 @@
 #!/usr/bin/env python3
 """Benchmark of the hot path: fp32 CSR SpMM C = A x B on one MI355X.
 
-    python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload conv|stress|ffn|ffn-all|matrix|sweep|narrow|sparsity|ablation|tune|unhinted|paths|parts]
+    python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload conv|stress|ffn|ffn-all|matrix|sweep|narrow|sparsity|ablation|tune|unhinted|paths|parts|block]
 
 A step is one pass of the whole hot path (spmm_execute, every kernel it
 launches) over the workload's column counts, with the plan and all operands
@@ -32,7 +32,8 @@ and three group budgets forced per matrix: what the closed schedule rule loses
 against the best candidate, and the plan's size against CSR and dense), `unhinted` (what the
 bCols hint is worth), `paths` (chunks against tiles of every panel height, with the two estimates
 between which a plan's path is chosen) and `parts` (tiles on bf16 parts: error against 64 bits beside that of fp32
-instructions, and times where the operands hold tiny or infinite values).
+instructions, and times where the operands hold tiny or infinite values) and `block` (feed-forward blocks, norm to second
+product, with 4-bit weights and with pruned ones).
 """
 import argparse
 import json
@@ -1104,6 +1105,68 @@ def run_parts(args):
                       "config": {"workload": "%d products on panels of 32 rows" % len(errors), "seed": args.seed}, "errors": errors, "times": times}))
 
 
+BLOCK_TOKENS = (1, 8, 32, 128)
+
+
+def block_passes(torch, spmm, gen, K, F, tokens):
+    """A pass of a feed-forward block of width K and inner width F on `tokens` tokens: the norm with the residual's
+    addition, the products of gate and up rows, the gated activation, the product back.  {"codes": 4-bit weights, 8-bit
+    codes between the operators, bfloat16 outside, one token a row of memory; "pruned": weights 70 % pruned (lognormal
+    rows), float32 columns}, the plans, and the arguments' device memory."""
+    g = torch.Generator(device="cuda").manual_seed(31 * K + tokens)
+    x, r = (torch.randn((tokens, K), device="cuda", generator=g) for _ in range(2))
+    w = torch.ones((K,), device="cuda")
+    up, down = (spmm.quant_plan_create(M, C, *gen.weights_4bit(M, C, 128, 7 * M + C), group=128) for M, C in ((2 * F, K), (K, F)))
+    xb, rb, wb = x.bfloat16().t(), r.bfloat16().t(), w.bfloat16()
+
+    def codes():
+        n = spmm.norm(xb, wb, residual=rb, dtype=torch.int8)
+        h = up.execute(n.out, scales=n.scales, dtype=torch.bfloat16)
+        z = spmm.gate(h[:F], h[F:], dtype=torch.int8)
+        return down.execute(z.out, scales=z.scales, dtype=torch.bfloat16), n.total
+
+    sparse = [gen.lognormal_rows(M, C, 0.7, 11 * M + C + i) for i, (M, C) in enumerate(((F, K), (F, K), (K, F)))]
+    plans = [spmm.plan_create(a.M, a.K, a.row_ptr, a.col_idx, a.vals, n_hint=tokens) for a in sparse]
+    xc, rc = x.t().contiguous(), r.t().contiguous()
+
+    def pruned():
+        n = spmm.norm(xc, w, residual=rc)
+        z = spmm.gate(plans[0].execute(n.out), plans[1].execute(n.out))
+        return plans[2].execute(z.out), n.total
+
+    return {"codes": codes, "pruned": pruned}, [up, down] + plans
+
+
+def run_block(args):
+    """Feed-forward blocks of the feed-forward shapes' sizes; a step is one pass at every token count."""
+    import torch
+    import paper_2506_15174_amd as spmm
+    from workloads import generators as gen
+    torch.cuda.set_device(0)
+    K, F = 1024, 4096
+    points, made = [], [(N,) + block_passes(torch, spmm, gen, K, F, N) for N in BLOCK_TOKENS]
+    for N, passes, _ in made:
+        point = {"tokens": N}
+        for name, call in passes.items():
+            for _ in range(args.warmup):
+                call()
+            torch.cuda.synchronize()
+            t0 = time.perf_counter()
+            for _ in range(args.steps):
+                call()
+            torch.cuda.synchronize()
+            point[name + "_us"] = round((time.perf_counter() - t0) / args.steps * 1e6, 3)
+        points.append(point)
+    us = sum(p["codes_us"] for p in points)
+    print(json.dumps({"metric": "tokens per second through a feed-forward block with 4-bit weights", "value": round(sum(BLOCK_TOKENS) / us * 1e6, 1),
+                      "unit": "tokens/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(us / 1e3, 5),
+                      "higher_is_better": True, "vs_baseline": None, "dtype": "bf16, int8 x int4", "data": "synthetic",
+                      "config": {"workload": "block of width %d, inner width %d, groups of 128 columns" % (K, F), "tokens": list(BLOCK_TOKENS)}, "points": points}))
+    for _, _, plans in made:
+        for plan in plans:
+            plan.destroy()
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -1111,7 +1174,7 @@ def main():
     ap.add_argument("--warmup", type=int, default=5)
     ap.add_argument("--workload", default="headline",
                     help="headline (default: sweep + stress) | conv | stress | ffn | ffn-all | matrix | sweep | "
-                         "narrow | sparsity | ablation | tune | unhinted | paths (--steps matrices) | parts")
+                         "narrow | sparsity | ablation | tune | unhinted | paths (--steps matrices) | parts | block")
     ap.add_argument("--shape", default="4096x4096", help="--workload matrix: rows x columns of A")
     ap.add_argument("--sparsity", type=float, default=0.5, help="--workload matrix: pruned share")
     ap.add_argument("--bcols", type=int, default=128, help="--workload matrix: columns of B")
@@ -1146,9 +1209,9 @@ def main():
         return run_sweep(args, cols=(64, 4), square512=True)
     if args.workload == "ffn-all":
         return run_sweep(args, ffn=True)
-    if args.workload in ("sweep", "ablation", "tune", "unhinted", "paths", "parts"):
+    if args.workload in ("sweep", "ablation", "tune", "unhinted", "paths", "parts", "block"):
         return {"sweep": run_sweep, "ablation": run_ablation, "tune": run_tune, "unhinted": run_unhinted,
-                "paths": run_paths, "parts": run_parts}[args.workload](args)
+                "paths": run_paths, "parts": run_parts, "block": run_block}[args.workload](args)
     return run_single(args)
 
 

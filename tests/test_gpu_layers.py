@@ -81,6 +81,15 @@ def test_whole_numbers_are_exact_in_every_shape_of_workgroup(type, group, M, K):
             check_product(M, K, N, group, type, "features", N + group + 1, whole=True)
 
 
+@pytest.mark.parametrize("type", ["float16", "bfloat16"])
+@pytest.mark.parametrize("group,zeros", [(32, True), (32, False), (64, True), (64, False), (128, True), (128, False)])
+@pytest.mark.parametrize("N", [2040, 1001, 500])
+def test_whole_numbers_are_exact_in_prompts(type, group, zeros, N):
+    """Teams of eight, four and two waves (the token counts); fewer blocks of columns than teams, as many, and more."""
+    for n, K in enumerate((100, 390, 650, 1300)):
+        check_product(4090 - 16 * n, K, N, group, type, ("tokens", "features")[n % 2], N + group, whole=True, zeros=zeros)
+
+
 @pytest.mark.parametrize("type", FLOATS + ("int8",))
 @pytest.mark.parametrize("M,K,N,group", [(1, 1, 1, 32), (1, 1, 5, 64), (5, 2, 1, 128), (16, 128, 16, 32), (17, 33, 2, 32), (33, 129, 33, 128), (64, 65, 64, 64),
                                          (100, 1000, 1, 128), (300, 257, 129, 384), (31, 4100, 7, 128), (48, 640, 300, 1024), (2100, 96, 8, 64), (130, 2048, 513, 64)])
@@ -428,6 +437,58 @@ def test_streams_and_graphs(N):
             for o, w in zip(outs[k], wants[k]):
                 assert torch.equal(o, w)
         assert torch.equal(eager[0], wants[0][0])
+
+
+@pytest.mark.parametrize("type", FLOATS)
+@pytest.mark.parametrize("D,N", [(1024, 128), (3000, 270), (5000, 2)])
+def test_rows_of_features_in_graphs(type, D, N):
+    """Norm and gate with a feature a row of memory: two graphs replayed in turn with eager calls on other sizes between them."""
+    inputs = [norm_case(D, N, type, "features", s) for s in (1, 2)]
+    other = norm_case(700, 400, type, "features", 3)
+
+    def calls(x, r, w):
+        n, c = spmm.norm(x, w, residual=r), spmm.norm(x, w, dtype=torch.int8)
+        g = spmm.gate(n.out, x, dtype=torch.int8)
+        return [n.out, n.total, c.out, c.scales, g.out, g.scales]
+
+    wants = [[o.clone() for o in calls(*i)] for i in inputs]
+    calls(*other)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for i in inputs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(calls(*i))
+        graphs.append(graph)
+    for _ in range(4):
+        for out in outs:
+            for o in out:
+                o.fill_(77)
+        graphs[1].replay()
+        calls(*other)
+        graphs[0].replay()
+        eager = calls(*inputs[0])
+        torch.cuda.synchronize()
+        for out, want in zip(outs + [eager], wants + wants[:1]):
+            for o, w in zip(out, want):
+                assert torch.equal(o, w)
+
+
+def test_the_benchmarks_blocks():
+    """Both blocks of the benchmark run, again with the same bits, and on one residual."""
+    import bench
+    from workloads import generators as gen
+    for tokens in (1, 24):
+        passes, plans = bench.block_passes(torch, spmm, gen, 128, 320, tokens)
+        (y, t), (z, u) = passes["codes"](), passes["pruned"]()
+        assert y.shape == z.shape == t.shape == u.shape == (128, tokens)
+        assert y.isfinite().all() and z.isfinite().all() and y.float().std() > 0 and z.std() > 0
+        # the sum of two values rounded to bf16, rounded: three half steps
+        assert ((t.float() - u).abs() <= 3 * 2.0 ** -8 * 1.01 * (u.abs() + 8)).all()
+        for name, want in (("codes", y), ("pruned", z)):
+            assert torch.equal(passes[name]()[0], want)
+        for plan in plans:
+            plan.destroy()
 
 
 def test_the_same_inputs_give_the_same_bits():

@@ -60,3 +60,16 @@ def test_what_creation_refuses():
     with pytest.raises(spmm.SpmmError) as err:
         spmm.quant_plan_create(6, 10, codes, scales, group=48)
     assert err.value.status == spmm.binding.SPMM_ERR_UNSUPPORTED
+
+
+def test_weights_of_the_benchmarks_blocks():
+    """Seeded, in the plan's form, and of the standard deviation that they are asked for."""
+    from workloads import generators as gen
+    codes, scales = gen.weights_4bit(64, 321, 128, 5)
+    assert codes.shape == (64, 161) and codes.dtype == np.uint8 and scales.shape == (64, 3) and scales.dtype == np.float32
+    again = gen.weights_4bit(64, 321, 128, 5)
+    assert np.array_equal(codes, again[0]) and np.array_equal(scales, again[1])
+    values = (codes & 15).astype(np.float64) - 8
+    values *= np.repeat(scales, 64, 1)[:, :161]
+    # uniform codes have a variance of 21.25 about -0.5, scales a mean square of 1.0133 (0.02 / 4.6)^2; 10304 draws are off by 5 % at most
+    assert abs(np.sqrt((values ** 2).mean()) / 0.02 - np.sqrt(21.5 * 1.0133) / 4.6) < 0.05

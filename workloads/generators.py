@@ -192,6 +192,15 @@ def activations_for(csr, N, seed_offset=0):
     return dense_activations(csr.K, N, 7919 * csr.K + 31 * N + 17 + seed_offset)
 
 
+def weights_4bit(M, K, group, seed, std=0.02):
+    """4-bit weights: uniform codes (two in a byte, the even column's in the low half) and a float32 scale a group, under
+    which weights have about the standard deviation std; the zero point is 8."""
+    rng = _rng(seed)
+    codes = rng.integers(0, 256, (M, (K + 1) // 2), dtype=np.uint8)
+    scales = rng.uniform(0.8, 1.2, (M, -(-K // group))) * std / 4.6
+    return codes, scales.astype(np.float32)
+
+
 def row_stats(csr):
     """Achieved nnz, mean / max row length and the Gini coefficient of the row
     lengths (reported with every measurement)."""
