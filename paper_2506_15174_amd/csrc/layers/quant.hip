@@ -7,7 +7,9 @@
 // (its 16 tokens are the rows of an instruction), W the second: a lane then holds four tokens of one row of W and
 // needs one scale a group.
 //
-// pack_kernel lays B out as the instructions take it; product_kernel gives a tile of 16 rows and up to 128 tokens to a workgroup, whose waves share K.
+// Up to 16 tokens, and somewhat more on short rows, go in one launch (direct_kernel): bound by a launch's few memory accesses, then by the weights' bytes.  More take two: pack_kernel
+// lays B out as the instructions take it, then many_kernel, bound by B's way through the vector L1, or, on prompts of 16-bit elements, wide_kernel, bound by the matrix cores and by
+// the instructions that make operands of weights.
 #include <algorithm>
 #include <hip/hip_runtime.h>
 
@@ -257,7 +259,8 @@ template <int BT> constexpr float WEIGHT_UNIT = BT == SPMM_F32 || BT == SPMM_BF1
 // ---- many tokens -----------------------------------------------------------------------------------------------
 //
 // A wave has RT tiles of rows and NT tiles of tokens, a workgroup KWAVES such waves that share K; their sums meet in LDS.  Weights become operands once a block and
-// are used for all of its tokens, B (laid out by pack_kernel) comes a tile of tokens at a time, the next one while one is multiplied.
+// are used for all of its tokens, B (laid out by pack_kernel) comes a tile of tokens at a time, the next one while one is multiplied.  With the layout of B: 4096 x 4096, 128 tokens
+// in bf16 14.8 us, 291 TF; 8192 x 8192, 512 in codes 73 us, 936 TF, in fp32 227 us, 303 TF (three products of bf16 for each).
 
 template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void many_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N,
                                                                                                                           tensor C)
@@ -407,8 +410,9 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 // A wave has 64 rows and 64 tokens.  Of a workgroup's eight, teams of SHARE lie one below the other and share the tokens' B; K is split over the 8 / SHARE teams, whose sums meet in LDS
 // at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock (1 KiB feeds four instructions of 16 clocks on each of four SIMDs); a
 // block of 128 columns is on its way there while the block before is multiplied.  A team waits for its own waves only: with a barrier for the workgroup 8192 x 8192, 512 tokens, took
-// 105 us, without 89 (teams of two).  Weights are made operands by each wave for itself: 52 instructions for 32 columns beside 16 of the matrix unit, two waves to a SIMD, is about what
-// keeps both busy.  In bf16, with 6 us to lay out B for 512 tokens: 83 us, 825 TF; 4096 tokens 586, 938 TF.
+// 105 us, without 89 (teams of two).  Weights are made operands by each wave for itself: 52 instructions for 32 columns beside 16 of the matrix unit, two waves to a SIMD;
+// the two kinds add up rather than overlap (a block takes 2.1 us in teams of eight: 0.9 of matrix instructions, 1.2 of others; interleaving them in the program's order gained nothing).
+// 8192 x 8192 in bf16, with 6 us to lay out B for 512 tokens: 512 84 us, 820 TF; 4096 586, 938 TF.
 
 constexpr int WIDE_TILES = 4, WIDE_STAGE = WIDE_TILES * 4096, WIDE_LDS = 8 * WIDE_TILES * WIDE_TILES * 1024;
 
@@ -526,7 +530,8 @@ template <int V> using constant = std::integral_constant<int, V>;
 // ---- in one launch ---------------------------------------------------------------------------------------------
 //
 // A product of few tokens is over in the time of a few memory accesses, of which a launch is two or three: every wave reads its columns of
-// B as it reads its weights and makes operands of them itself.  Lanes of tokens that do not exist read the last one's (an access the
+// B as it reads its weights and makes operands of them itself.  In bf16, one token: 4096 x 4096 4.3 us, 2.1 TB/s of weights and all; 8192 x 8192 10.4 us, 3.4 TB/s; 16384 x 16384
+// 36 us, 3.9 TB/s, where a large copy reaches 5.1.  Lanes of tokens that do not exist read the last one's (an access the
 // wave makes anyway); their results are not stored.  Weights, scales and B of AHEAD blocks are asked for before the first is used.
 //   PER_GROUP  steps of 32 columns behind which a group's sum is full (4, 2 or 1)
 //   RT, NT     tiles of rows and of tokens of a wave
@@ -807,10 +812,12 @@ template <int BT, int SHARE> hipError_t launch_wide(const quant_matrix &w, const
 }
 
 // On B laid out by pack_kernel.  Small tiles while they leave no compute unit without a workgroup; then larger ones, which read B and make operands of weights less often.
-// us, tiles of rows x of tokens of a wave (wide: wide_kernel), bf16:
-//   1024 x 4096, 128 tokens   1x2  9.4   2x2 10.8   2x4 13.2                 4096 x 4096, 128   1x2 17.0   2x2 14.7   2x4 14.0
-//   16384 x 4096, 64          1x2 33     2x2 26     2x4 27                   3001 x 2511, 200   1x2 15.5   2x2 14.8   2x4 18.8
-//   8192 x 8192, 256          2x2 70     2x4 67     wide 60                  8192 x 4096, 320   2x2 50     2x4 54     wide 58 (320 workgroups)
+// us, tiles of rows x of tokens of a wave (teams of two, four and eight waves: wide_kernel), bf16:
+//   1024 x 4096, 128 tokens   1x2  9.4   2x2 10.8   2x4 13.2                        4096 x 4096, 128    1x2 17.0   2x2 14.7   2x4 14.0   two 25.3
+//   16384 x 4096, 64          1x2 33     2x2 26     2x4 27     two 28               3001 x 2511, 200    1x2 15.5   2x2 14.7   2x4 18.8   two 20.4
+//   8192 x 8192, 128          2x2 40     two 42     four 73                         8192 x 8192, 192    2x2 56     two 45     four 74
+//   8192 x 8192, 320          2x2 90     two 81     four 76    eight 141            8192 x 8192, 2048   2x2 513    two 335    four 312   eight 296
+//   16384 x 4096, 300         2x2 91     two 76     four 83    eight 82             1024 x 1024, 8192   2x2 57     two 59     four 49    eight 41
 // in codes: 8192 x 8192, 256 2x2 53, 4x4 41; 2048 x 8192, 512 2x2 28, 4x4 35 (256 workgroups)
 // in fp32: 4096 x 4096, 128 2x2 26, 2x4 23, 4x4 34; 4096 x 4096, 256 2x2 47, 2x4 42, 4x4 36
 template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)

@@ -7,7 +7,9 @@
 //
 // Codes do not wait for f: they depend on p alone, so one look at the token gives both statistics.  All of it is bound by
 // memory, or by the latency of one launch: elements are read once and held in registers between the statistics
-// and the output where registers hold them.
+// and the output where registers hold them.  With the residual's addition, us (of which a launch is 2.4): one token of 4096 in bf16 3.3; 2048 tokens of 8192 in bf16 28, 4.8 TB/s, in codes 27;
+// where a row of memory is a feature, fp32, 128 tokens of 1024 6.9, 2048 tokens of 4096 47, 2.9 TB/s (3.6 with the sum's second reading).  The gate: 16 tokens of 4096 in f16 2.6; 2048 of
+// 16384 in bf16 37, 5.5 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -441,11 +443,13 @@ template <int TYPE> hipError_t launch_elements(const rows_args &a, hipStream_t s
     return launch_kernel(elements_kernel<TYPE>, grid_of((rows * units + 255) / 256), 256, 0, stream, a, rows, length, (uint32_t)units);
 }
 
-// One launch beats two where a workgroup's registers hold its tokens and few workgroups read the same lines: 0, or the threads side by side.
+// One launch, whose workgroups have all features of their tokens, or two, as far as a workgroup's registers hold its tokens and few workgroups read the same lines: 0, or the threads side by side.
+// us of one thread, 64 bytes side by side and two launches, K x N in fp32: 1024 x 32 4.8, 6.8, 7.7; 1024 x 128 7.7, 6.9, 7.7; 1024 x 256 9.4, 10.1, 8.7; 300 x 1000 7.4, 6.6, 10.2;
+// 4096 x 8 7.6, -, 8.7; 4096 x 16 13.7, -, 8.3; 4096 x 256 34, -, 10.5.  bf16: 1024 x 64 6.5, 7.2, 9.9; 1024 x 256 10.0, 9.9, 10.0; 2048 x 32 8.0, -, 10.6; 4096 x 16 8.1, -, 11.1; 4096 x 64 18, -, 10.7.
 int in_one_launch(int64_t K, int64_t N, int unit)
 {
-    if (K <= 4 * COLUMN_THREADS && N <= 32) return 1;
-    return K <= 4 * COLUMN_THREADS / (16 / unit) && N <= 256 ? 16 / unit : 0;
+    if (K <= 4 * COLUMN_THREADS && K * N <= 8192 * unit) return 1;
+    return K <= COLUMN_THREADS && N <= (K <= 512 ? 1024 : 32 * unit) ? 16 / unit : 0;
 }
 
 // Tiles of AT_ONCE steps of rows, or as many as leave 64 in a column; whole pieces of codes.
@@ -486,7 +490,7 @@ template <bool NORM, bool CODES, int TYPE> hipError_t launch(const rows_args &a,
     if (units <= 64) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 64, 1, 4>, grid_of((N + 3) / 4), 256, 0, stream, a);
     if (units <= 256) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 256, 1, 1>, grid_of(N), 256, 0, stream, a);
     // Few tokens are over when their slowest is: more threads each.  Many are a matter of bandwidth, which smaller workgroups, of which a compute unit has
-    // several in different phases, come nearer to.
+    // several in different phases, come nearer to.  us with 1024 threads and with 256, bf16: 8192 x 16 3.5 and 5.2, x 512 8.8 and 9.9, x 1024 16.2 and 14.9; 4096 x 4096 34 and 27.
     const bool few = N <= 512;
     if (units <= 512 && !few) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 256, 2, 1>, grid_of(N), 256, 0, stream, a);
     if (units <= 1024 && !few) return launch_kernel(rows_kernel<NORM, CODES, TYPE, 256, 4, 1>, grid_of(N), 256, 0, stream, a);
