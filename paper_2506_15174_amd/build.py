@@ -4,6 +4,7 @@
 
 Output: paper_2506_15174_amd/lib/libspmm_cdna4.so (C ABI of include/spmm.h).
 """
+import concurrent.futures
 import os
 import shutil
 import subprocess
@@ -139,8 +140,8 @@ def build(verbose=False):
     hipcc = _hipcc()
     common = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-Wno-unused-parameter",
               "-I", CSRC, "-I", os.path.join(ROCM, "include"), "-D__HIP_PLATFORM_AMD__=1"]
-    objects = []
-    for s in SOURCES:
+
+    def compiled(s):
         obj = os.path.join(obj_dir, os.path.splitext(s)[0].replace("/", "_") + ".o")
         if s.endswith(".hip"):
             cmd = [hipcc, "--offload-arch=gfx950",
@@ -164,7 +165,10 @@ def build(verbose=False):
                 raise RuntimeError("%s: of the barriers behind a strip's copy, one in each kernel, %d were found" % (s, n))
             if verbose:
                 print("%s: %d barriers that loads may cross, none of them to LDS" % (s, n))
-        objects.append(obj)
+        return obj
+
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:  # (a compiler each)
+        objects = list(pool.map(compiled, sorted(SOURCES, key=lambda s: s != "layers/quant.hip")))  # the longest first
     _run([hipcc, "-shared", "-fPIC"] + objects +
          ["-L", os.path.join(ROCM, "lib"), "-lamdhip64", "-pthread", "-o", LIB_PATH], verbose)
     build_torch_extension(verbose)
