@@ -160,6 +160,16 @@ def test_nothing_to_do():
         assert plan.describe() == {"M": M, "K": K, "group": 128, "device_bytes": 0}
 
 
+@pytest.mark.parametrize("type", FLOATS + ("int8",))
+@pytest.mark.parametrize("M,N", [(70, 300), (4090, 1000), (20, 17)])
+def test_no_columns_and_many_tokens(type, M, N):
+    plan = spmm.quant_plan_create(M, 0, np.zeros((M, 0), np.uint8), np.zeros((M, 0), np.float32))
+    B = torch.zeros((0, N), dtype=TYPES[type], device="cuda")
+    C = torch.full((M, N), 7.0, device="cuda")
+    plan.execute(B, C=C, scales=torch.ones(N, device="cuda") if type == "int8" else None)
+    assert (C == 0).all()
+
+
 def test_plans_from_tensors_of_every_kind():
     codes, scales, zeros, W = weights(20, 70, 32, 5, whole=True)
     B = torch.randint(-3, 4, (70, 9)).float()
@@ -489,6 +499,35 @@ def test_the_benchmarks_blocks():
             assert torch.equal(passes[name]()[0], want)
         for plan in plans:
             plan.destroy()
+
+
+@pytest.mark.parametrize("order", ["tokens", "features"])
+@pytest.mark.parametrize("K,N", [(48, 3), (48, 40), (300, 8), (2, 100)])
+def test_offsets_past_32_bits(order, K, N):
+    """Rows of memory that lie 2^32 elements apart, first to last: the same bits as from rows that lie together."""
+    rows, row = (N, K) if order == "tokens" else (K, N)
+    ld = max(row, 2 ** 32 // (rows - 1) + 1)
+
+    def apart(like):
+        far = torch.empty(((rows - 1) * ld + row,), dtype=like.dtype, device="cuda").as_strided((rows, row), (ld, 1))
+        far.copy_(like if order == "features" else like.t())
+        return far if order == "features" else far.t()
+
+    x = torch.randn((K, N), device="cuda").bfloat16()
+    near = x if order == "features" else x.t().contiguous().t()
+    far, w = apart(x), torch.ones(K, device="cuda")
+    plan, _ = plan_of(50, K, 64, 3)
+    assert torch.equal(plan.execute(far), plan.execute(near))
+    out = apart(torch.zeros_like(x))
+    n, m = spmm.norm(far, w, residual=near, out=out), spmm.norm(near, w, residual=near)
+    assert n.out is out and torch.equal(out, m.out) and torch.equal(n.total, m.total)
+    for dtype in (torch.bfloat16, torch.int8):
+        g, h = spmm.gate(far, near, dtype=dtype), spmm.gate(near, near, dtype=dtype)
+        assert torch.equal(g.out, h.out) and (dtype != torch.int8 or torch.equal(g.scales, h.scales))
+    if order == "tokens":
+        q = torch.randint(-127, 128, (K, N), dtype=torch.int8, device="cuda")
+        s = torch.rand(N, device="cuda")
+        assert torch.equal(plan.execute(apart(q), scales=s), plan.execute(q.t().contiguous().t(), scales=s))
 
 
 def test_the_same_inputs_give_the_same_bits():
