@@ -407,21 +407,22 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 
 // ---- prompts -----------------------------------------------------------------------------------------------------
 //
-// A wave has 64 rows and 64 tokens.  Of a workgroup's eight, teams of SHARE lie one below the other and share the tokens' B; K is split over the 8 / SHARE teams, whose sums meet in LDS
-// at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock (1 KiB feeds four instructions of 16 clocks on each of four SIMDs); a
-// block of 128 columns is on its way there while the block before is multiplied.  A team waits for its own waves only: with a barrier for the workgroup 8192 x 8192, 512 tokens, took
-// 105 us, without 89 (teams of two).  Weights are made operands by each wave for itself: 52 instructions for 32 columns beside 16 of the matrix unit, two waves to a SIMD;
-// the two kinds add up rather than overlap (a block takes 2.1 us in teams of eight: 0.9 of matrix instructions, 1.2 of others; interleaving them in the program's order gained nothing).
-// 8192 x 8192 in bf16, with 6 us to lay out B for 512 tokens: 512 84 us, 820 TF; 4096 586, 938 TF.
+// A wave has 16 tiles of sums, NT of tokens beside 16 / NT of rows.  Of a workgroup's eight, teams of SHARE lie one below the other and share the tokens' B; K is split over the
+// 8 / SHARE teams, whose sums meet in LDS at the end.  B goes through LDS, since without sharing it would take all of the vector L1's 64 bytes a clock; a block of 128 columns is on its
+// way there while the block before is multiplied.  A team waits for its own waves only: with a barrier for the workgroup 8192 x 8192, 512 tokens, took 105 us, without 89 (teams of two;
+// a second block on its way, with which waves of a team may be a block apart, gained nothing).  Weights are made operands by each wave for itself, 13 instructions for a tile of rows and
+// 32 columns, which matrix instructions share with NT tiles of tokens: 128 tokens a wave instead of 64 take 81 us and 83, in teams of eight 142 and 150 on 1024 (LDS does not hold
+// them for teams of two).  Two waves a SIMD issue an instruction of that kind in 4.8 clocks, and what both kinds take adds up rather than overlaps, also where the program interleaves them.
+// 8192 x 8192 in bf16, with 6 us to lay out B for 512 tokens: 512 81 us, 850 TF; 4096 546, 1006 TF.
 
-constexpr int WIDE_TILES = 4, WIDE_STAGE = WIDE_TILES * 4096, WIDE_LDS = 8 * WIDE_TILES * WIDE_TILES * 1024;
+constexpr int WIDE_LDS = 128 * 1024;
 
-template <int BT, int SHARE, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, int64_t N, tensor C)
+template <int BT, int SHARE, int NT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, int64_t N, tensor C)
 {
     static_assert(BT == SPMM_F16 || BT == SPMM_BF16);
     extern __shared__ __align__(16) char lds[];
-    constexpr int TEAMS = 8 / SHARE, RT = WIDE_TILES, NT = WIDE_TILES, SUMS = 4 / STEPS, BLOCK_BYTES = 4 * STEP_BYTES<BT>, EACH = WIDE_STAGE / 1024 / SHARE;
-    static_assert(BLOCK_BYTES * NT == WIDE_STAGE && 2 * TEAMS * WIDE_STAGE <= WIDE_LDS);
+    constexpr int TEAMS = 8 / SHARE, RT = 16 / NT, SUMS = 4 / STEPS, BLOCK_BYTES = 4 * STEP_BYTES<BT>, STAGE = NT * BLOCK_BYTES, EACH = STAGE / 1024 / SHARE;
+    static_assert(BLOCK_BYTES == 4096 && 2 * TEAMS * STAGE <= WIDE_LDS && 8 * RT * NT * 1024 == WIDE_LDS && RT <= TILES_OF);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
     const int member = wave % SHARE, team = wave / SHARE;
     const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * NT, wg_tile0 = (int64_t)blockIdx.x * (SHARE * RT);
@@ -444,7 +445,7 @@ template <int BT, int SHARE, int STEPS, bool ZEROS> __global__ __launch_bounds__
         }
     };
     // This wave's share of a block of B, straight to LDS: [place][team][tile of tokens][4 KiB each]
-    auto place_of = [&](int place) { return lds + (place * TEAMS + team) * WIDE_STAGE; };
+    auto place_of = [&](int place) { return lds + (place * TEAMS + team) * STAGE; };
     auto send = [&](int b, int place) {
 #pragma unroll
         for (int l = 0; l < EACH; ++l) {
@@ -475,7 +476,7 @@ template <int BT, int SHARE, int STEPS, bool ZEROS> __global__ __launch_bounds__
         const char *const from = place_of(round & 1) + lane * 16;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            if (STEPS < 4) __builtin_amdgcn_sched_barrier(0);  // (scales of several groups: no registers for two steps at a time)
+            if (STEPS < 4 || (BT == SPMM_F16 && ZEROS)) __builtin_amdgcn_sched_barrier(0);  // (scales of several groups, zero points in f16: no registers for two steps at a time)
             u32x4 w[RT], x[NT];
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
@@ -507,7 +508,6 @@ template <int BT, int SHARE, int STEPS, bool ZEROS> __global__ __launch_bounds__
     __syncthreads();
     float *const sums = reinterpret_cast<float *>(lds);
     constexpr int ROW_TILES = SHARE * RT;
-    static_assert(TEAMS * ROW_TILES * NT * 1024 == WIDE_LDS);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -798,13 +798,14 @@ template <int BT, int NT, int RT, int KWAVES> hipError_t launch_many(const quant
     return run(constant<4>());
 }
 
-template <int BT, int SHARE> hipError_t launch_wide(const quant_matrix &w, const char *B, int64_t N, const tensor &C, hipStream_t stream)
+template <int BT, int SHARE, int NT> hipError_t launch_wide(const quant_matrix &w, const char *B, int64_t N, const tensor &C, hipStream_t stream)
 {
-    const dim3 blocks((unsigned)((w.tiles + SHARE * WIDE_TILES - 1) / (SHARE * WIDE_TILES)), (unsigned)((N + 16 * WIDE_TILES - 1) / (16 * WIDE_TILES)));
+    constexpr int ROWS = SHARE * (16 / NT);
+    const dim3 blocks((unsigned)((w.tiles + ROWS - 1) / ROWS), (unsigned)((N + 16 * NT - 1) / (16 * NT)));
     auto run = [&](auto per_group) {
         constexpr int PER_GROUP = decltype(per_group)::value;
-        if (w.zeros) return launch_kernel(wide_kernel<BT, SHARE, PER_GROUP, true>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
-        return launch_kernel(wide_kernel<BT, SHARE, PER_GROUP, false>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
+        if (w.zeros) return launch_kernel(wide_kernel<BT, SHARE, NT, PER_GROUP, true>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
+        return launch_kernel(wide_kernel<BT, SHARE, NT, PER_GROUP, false>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
     };
     if (w.group == 32) return run(constant<1>());
     if (w.group == 64) return run(constant<2>());
@@ -815,9 +816,9 @@ template <int BT, int SHARE> hipError_t launch_wide(const quant_matrix &w, const
 // us, tiles of rows x of tokens of a wave (teams of two, four and eight waves: wide_kernel), bf16:
 //   1024 x 4096, 128 tokens   1x2  9.4   2x2 10.8   2x4 13.2                        4096 x 4096, 128    1x2 17.0   2x2 14.7   2x4 14.0   two 25.3
 //   16384 x 4096, 64          1x2 33     2x2 26     2x4 27     two 28               3001 x 2511, 200    1x2 15.5   2x2 14.7   2x4 18.8   two 20.4
-//   8192 x 8192, 128          2x2 40     two 42     four 73                         8192 x 8192, 192    2x2 56     two 45     four 74
-//   8192 x 8192, 320          2x2 90     two 81     four 76    eight 141            8192 x 8192, 2048   2x2 513    two 335    four 312   eight 296
-//   16384 x 4096, 300         2x2 91     two 76     four 83    eight 82             1024 x 1024, 8192   2x2 57     two 59     four 49    eight 41
+//   8192 x 8192, 128          2x2 40     two 42     four 71                         8192 x 8192, 192    2x2 56     two 45     four 72
+//   8192 x 8192, 320          2x2 90     two 81     four 74    eight 126            8192 x 8192, 2048   2x2 513    two 335    four 309   eight 275
+//   16384 x 4096, 300         2x2 91     two 75     four 81    eight 74             1024 x 1024, 8192   2x2 57     two 59     four 52    eight 42
 // in codes: 8192 x 8192, 256 2x2 53, 4x4 41; 2048 x 8192, 512 2x2 28, 4x4 35 (256 workgroups)
 // in fp32: 4096 x 4096, 128 2x2 26, 2x4 23, 4x4 34; 4096 x 4096, 256 2x2 47, 2x4 42, 4x4 36
 template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
@@ -830,13 +831,13 @@ template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, 
     } else if constexpr (BT == SPMM_I8) {
         if (workgroups(4, 4) >= 480) return launch_many<BT, 4, 4, 4>(w, B, B_scales, N, C, stream);
     } else {
-        // Rounds of 256 workgroups, by what one takes (of 8192 columns 8, 41, 76 and 137 us): the fewer rows a team has, the more often B is read.
+        // Rounds of 256 workgroups, by what one takes (of 8192 columns 8, 41, 74 and 124 us): the fewer rows a team has, the more often B is read.
         auto us = [&](int64_t rows, int64_t tokens, int64_t round) { return (workgroups(rows, tokens) + 255) / 256 * round; };
-        const int64_t two = us(8, 4, 41), four = us(16, 4, 76), eight = us(32, 4, 137);
+        const int64_t two = us(8, 4, 41), four = us(8, 8, 74), eight = us(16, 8, 124);
         if (std::min({two, four, eight}) < us(2, 2, 8)) {
-            if (eight <= std::min(two, four)) return launch_wide<BT, 8>(w, B, N, C, stream);
-            if (four <= two) return launch_wide<BT, 4>(w, B, N, C, stream);
-            return launch_wide<BT, 2>(w, B, N, C, stream);
+            if (eight <= std::min(two, four)) return launch_wide<BT, 8, 8>(w, B, N, C, stream);
+            if (four <= two) return launch_wide<BT, 4, 8>(w, B, N, C, stream);
+            return launch_wide<BT, 2, 4>(w, B, N, C, stream);
         }
     }
     return launch_many<BT, 2, 2, 8>(w, B, B_scales, N, C, stream);
