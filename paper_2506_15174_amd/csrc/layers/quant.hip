@@ -8,7 +8,7 @@
 // needs one scale a group.
 //
 // Up to 16 tokens, and somewhat more on short rows, go in one launch (direct_kernel): bound by a launch's few memory accesses, then by the weights' bytes.  More take two: pack_kernel
-// lays B out as the instructions take it, then many_kernel, bound by B's way through the vector L1, or, on prompts of 16-bit elements, wide_kernel, bound by the matrix cores and by
+// lays B out as the instructions take it, then many_kernel, bound by B's way through the vector L1, or, on prompts of all but fp32, wide_kernel, bound by the matrix cores and by
 // the instructions that make operands of weights.
 #include <algorithm>
 #include <hip/hip_runtime.h>
@@ -260,7 +260,7 @@ template <int BT> constexpr float WEIGHT_UNIT = BT == SPMM_F32 || BT == SPMM_BF1
 //
 // A wave has RT tiles of rows and NT tiles of tokens, a workgroup KWAVES such waves that share K; their sums meet in LDS.  Weights become operands once a block and
 // are used for all of its tokens, B (laid out by pack_kernel) comes a tile of tokens at a time, the next one while one is multiplied.  With the layout of B: 4096 x 4096, 128 tokens
-// in bf16 14.8 us, 291 TF; 8192 x 8192, 512 in codes 73 us, 936 TF, in fp32 227 us, 303 TF (three products of bf16 for each).
+// in bf16 14.8 us, 291 TF; 8192 x 8192, 512 in fp32 227 us, 303 TF (three products of bf16 for each).
 
 template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void many_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N,
                                                                                                                           tensor C)
@@ -413,16 +413,15 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 // a second block on its way, with which waves of a team may be a block apart, gained nothing).  Weights are made operands by each wave for itself, 13 instructions for a tile of rows and
 // 32 columns, which matrix instructions share with NT tiles of tokens: 128 tokens a wave instead of 64 take 81 us and 83, in teams of eight 142 and 150 on 1024 (LDS does not hold
 // them for teams of two).  Two waves a SIMD issue an instruction of that kind in 4.8 clocks, and what both kinds take adds up rather than overlaps, also where the program interleaves them.
-// 8192 x 8192 in bf16, with 6 us to lay out B for 512 tokens: 512 81 us, 850 TF; 4096 546, 1006 TF.
+// 8192 x 8192 in bf16, with 6 us to lay out B for 512 tokens: 512 81 us, 850 TF; 4096 546, 1006 TF; in codes 512 60 us, 1150 TOPS, 2048 197 us, 1400 TOPS.
 
 constexpr int WIDE_LDS = 128 * 1024;
 
-template <int BT, int SHARE, int NT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, int64_t N, tensor C)
+template <int BT, int SHARE, int NT, int STEPS, bool ZEROS> __global__ __launch_bounds__(512) void wide_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N, tensor C)
 {
-    static_assert(BT == SPMM_F16 || BT == SPMM_BF16);
     extern __shared__ __align__(16) char lds[];
-    constexpr int TEAMS = 8 / SHARE, RT = 16 / NT, SUMS = 4 / STEPS, BLOCK_BYTES = 4 * STEP_BYTES<BT>, STAGE = NT * BLOCK_BYTES, EACH = STAGE / 1024 / SHARE;
-    static_assert(BLOCK_BYTES == 4096 && 2 * TEAMS * STAGE <= WIDE_LDS && 8 * RT * NT * 1024 == WIDE_LDS && RT <= TILES_OF);
+    constexpr int TEAMS = 8 / SHARE, RT = 16 / NT, SUMS = 4 / STEPS, BLOCK_BYTES = 4 * STEP_BYTES<BT>, OF_TILE = BLOCK_BYTES / 1024, STAGE = NT * BLOCK_BYTES, EACH = STAGE / 1024 / SHARE;
+    static_assert(BT != SPMM_F32 && EACH * SHARE == NT * OF_TILE && 2 * TEAMS * STAGE <= WIDE_LDS && 8 * RT * NT * 1024 == WIDE_LDS && RT <= TILES_OF);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
     const int member = wave % SHARE, team = wave / SHARE;
     const int64_t token_tiles = (N + 15) / 16, token0 = (int64_t)blockIdx.y * NT, wg_tile0 = (int64_t)blockIdx.x * (SHARE * RT);
@@ -444,22 +443,25 @@ template <int BT, int SHARE, int NT, int STEPS, bool ZEROS> __global__ __launch_
             a.span[i] = span_of<SUMS, ZEROS>(W, tile0 + i, b, r);
         }
     };
-    // This wave's share of a block of B, straight to LDS: [place][team][tile of tokens][4 KiB each]
+    // This wave's share of a block of B, straight to LDS: [place][team][tile of tokens][a block of it]
     auto place_of = [&](int place) { return lds + (place * TEAMS + team) * STAGE; };
     auto send = [&](int b, int place) {
 #pragma unroll
         for (int l = 0; l < EACH; ++l) {
             const int at = member * EACH + l;
-            const char *from = B + (min(token0 + at / 4, token_tiles - 1) * W.blocks + b) * BLOCK_BYTES + at % 4 * 1024 + lane * 16;
+            const char *from = B + (min(token0 + at / OF_TILE, token_tiles - 1) * W.blocks + b) * BLOCK_BYTES + at % OF_TILE * 1024 + lane * 16;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)(place_of(place) + at * 1024), 16, 0, 0);
         }
     };
-    f32x4 acc[RT][NT], part[RT][NT];
+    typedef std::conditional_t<BT == SPMM_I8, i32x4, f32x4> sum;
+    f32x4 acc[RT][NT];
+    sum part[RT][NT];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
     asked now, next;
+    constexpr int AT_ONCE = BT == SPMM_I8 && STEPS > 1 ? 2 : 1;  // steps that go into one instruction
     if (first < last) {
         send(first, 0);
         ask(first, now);
@@ -475,31 +477,53 @@ template <int BT, int SHARE, int NT, int STEPS, bool ZEROS> __global__ __launch_
         if (b + 1 < last) send(b + 1, (round + 1) & 1);
         const char *const from = place_of(round & 1) + lane * 16;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            if (STEPS < 4 || (BT == SPMM_F16 && ZEROS)) __builtin_amdgcn_sched_barrier(0);  // (scales of several groups, zero points in f16: no registers for two steps at a time)
-            u32x4 w[RT], x[NT];
+        for (int s = 0; s < 4; s += AT_ONCE) {
+            // (scales of several groups, zero points in f16: no registers for two steps at a time)
+            if (STEPS < 4 || (BT == SPMM_F16 && ZEROS)) __builtin_amdgcn_sched_barrier(0);
+            if constexpr (BT == SPMM_I8) {
+                i32x4 x[NT];
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                if constexpr (BT == SPMM_F16) w[i] = __builtin_bit_cast(u32x4, weights_f16(now.word[i][s], now.span[i].zero(s / STEPS)));
-                else w[i] = __builtin_bit_cast(u32x4, weights_bf16<ZEROS>(now.word[i][s], now.span[i].zero(s / STEPS)));
-            }
+                for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const i32x4 *>(from + t * BLOCK_BYTES + s / 2 * 1024);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const u32x4 *>(from + t * BLOCK_BYTES + s * 1024);
+                for (int i = 0; i < RT; ++i) {
+                    const u32x2 w0 = weights_i8(now.word[i][s], (uint32_t)now.span[i].zero(s / STEPS) * 0x01010101u);
+                    if constexpr (STEPS == 1) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+                        for (int t = 0; t < NT; ++t)
+                            part[i][t] = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)((uint64_t)(uint32_t)x[t][2 * (s % 2)] | (uint64_t)(uint32_t)x[t][2 * (s % 2) + 1] << 32),
+                                                                               __builtin_bit_cast(long, w0), sum{0, 0, 0, 0}, 0, 0, 0);
+                    } else {
+                        const u32x2 w1 = weights_i8(now.word[i][s + 1], (uint32_t)now.span[i].zero(s / STEPS) * 0x01010101u);
+                        const i32x4 w = {(int)w0[0], (int)w0[1], (int)w1[0], (int)w1[1]};
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const f32x4 c = s % STEPS == 0 ? f32x4{0, 0, 0, 0} : part[i][t];
-                    if constexpr (BT == SPMM_F16) part[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[t]), __builtin_bit_cast(f16x8, w[i]), c, 0, 0, 0);
-                    else part[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, w[i]), c, 0, 0, 0);
+                        for (int t = 0; t < NT; ++t) part[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w, s % STEPS == 0 ? sum{0, 0, 0, 0} : part[i][t], 0, 0, 0);
+                    }
                 }
-            if (s % STEPS == STEPS - 1) {
+            } else {
+                u32x4 w[RT], x[NT];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    if constexpr (BT == SPMM_F16) w[i] = __builtin_bit_cast(u32x4, weights_f16(now.word[i][s], now.span[i].zero(s / STEPS)));
+                    else w[i] = __builtin_bit_cast(u32x4, weights_bf16<ZEROS>(now.word[i][s], now.span[i].zero(s / STEPS)));
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const u32x4 *>(from + t * BLOCK_BYTES + s * 1024);
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const sum c = s % STEPS == 0 ? sum{0, 0, 0, 0} : part[i][t];
+                        if constexpr (BT == SPMM_F16) part[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[t]), __builtin_bit_cast(f16x8, w[i]), c, 0, 0, 0);
+                        else part[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, w[i]), c, 0, 0, 0);
+                    }
+            }
+            if ((s + AT_ONCE) % STEPS == 0) {
 #pragma unroll
                 for (int i = 0; i < RT; ++i)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][t][e] += now.span[i].scale[s / STEPS] * WEIGHT_UNIT<BT> * part[i][t][e];
+                        for (int e = 0; e < 4; ++e) acc[i][t][e] += now.span[i].scale[s / STEPS] * WEIGHT_UNIT<BT> * (float)part[i][t][e];
             }
         }
         now = next;
@@ -521,6 +545,7 @@ template <int BT, int SHARE, int NT, int STEPS, bool ZEROS> __global__ __launch_
         float v = 0.0f;
 #pragma unroll
         for (int k = 0; k < TEAMS; ++k) v += sums[k * ROW_TILES * NT * 256 + at];
+        if (BT == SPMM_I8) v *= B_scales[n];
         store_as(C.data, C.by_token ? n * C.ld + row : row * C.ld + n, C.type, v);
     }
 }
@@ -798,14 +823,14 @@ template <int BT, int NT, int RT, int KWAVES> hipError_t launch_many(const quant
     return run(constant<4>());
 }
 
-template <int BT, int SHARE, int NT> hipError_t launch_wide(const quant_matrix &w, const char *B, int64_t N, const tensor &C, hipStream_t stream)
+template <int BT, int SHARE, int NT> hipError_t launch_wide(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
     constexpr int ROWS = SHARE * (16 / NT);
     const dim3 blocks((unsigned)((w.tiles + ROWS - 1) / ROWS), (unsigned)((N + 16 * NT - 1) / (16 * NT)));
     auto run = [&](auto per_group) {
         constexpr int PER_GROUP = decltype(per_group)::value;
-        if (w.zeros) return launch_kernel(wide_kernel<BT, SHARE, NT, PER_GROUP, true>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
-        return launch_kernel(wide_kernel<BT, SHARE, NT, PER_GROUP, false>, blocks, 512, WIDE_LDS, stream, w, B, N, C);
+        if (w.zeros) return launch_kernel(wide_kernel<BT, SHARE, NT, PER_GROUP, true>, blocks, 512, WIDE_LDS, stream, w, B, B_scales, N, C);
+        return launch_kernel(wide_kernel<BT, SHARE, NT, PER_GROUP, false>, blocks, 512, WIDE_LDS, stream, w, B, B_scales, N, C);
     };
     if (w.group == 32) return run(constant<1>());
     if (w.group == 64) return run(constant<2>());
@@ -819,7 +844,8 @@ template <int BT, int SHARE, int NT> hipError_t launch_wide(const quant_matrix &
 //   8192 x 8192, 128          2x2 40     two 42     four 71                         8192 x 8192, 192    2x2 56     two 45     four 72
 //   8192 x 8192, 320          2x2 90     two 81     four 74    eight 126            8192 x 8192, 2048   2x2 513    two 335    four 309   eight 275
 //   16384 x 4096, 300         2x2 91     two 75     four 81    eight 74             1024 x 1024, 8192   2x2 57     two 59     four 52    eight 42
-// in codes: 8192 x 8192, 256 2x2 53, 4x4 41; 2048 x 8192, 512 2x2 28, 4x4 35 (256 workgroups)
+// in codes: 8192 x 8192, 128 2x2 30, two 34; 256 2x2 53, 4x4 42, two 37; 512 4x4 74, two 67, four 60, eight 96; 2048 4x4 260, two 246, four 210, eight 197;
+//   2048 x 8192, 512 2x2 28, two 34; with groups of 32 and zero points 8192 x 8192, 512 4x4 235, four 101
 // in fp32: 4096 x 4096, 128 2x2 26, 2x4 23, 4x4 34; 4096 x 4096, 256 2x2 47, 2x4 42, 4x4 36
 template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, const float *B_scales, int64_t N, const tensor &C, hipStream_t stream)
 {
@@ -828,16 +854,15 @@ template <int BT> hipError_t execute_many(const quant_matrix &w, const char *B, 
     if constexpr (BT == SPMM_F32) {
         if (workgroups(4, 4) >= 180) return launch_many<BT, 4, 4, 4>(w, B, B_scales, N, C, stream);
         if (workgroups(2, 4) >= 180) return launch_many<BT, 4, 2, 8>(w, B, B_scales, N, C, stream);
-    } else if constexpr (BT == SPMM_I8) {
-        if (workgroups(4, 4) >= 480) return launch_many<BT, 4, 4, 4>(w, B, B_scales, N, C, stream);
     } else {
-        // Rounds of 256 workgroups, by what one takes (of 8192 columns 8, 41, 74 and 124 us): the fewer rows a team has, the more often B is read.
+        // Rounds of 256 workgroups, by what one takes (of 8192 columns): the fewer rows a team has, the more often B is read.
         auto us = [&](int64_t rows, int64_t tokens, int64_t round) { return (workgroups(rows, tokens) + 255) / 256 * round; };
-        const int64_t two = us(8, 4, 41), four = us(8, 8, 74), eight = us(16, 8, 124);
-        if (std::min({two, four, eight}) < us(2, 2, 8)) {
-            if (eight <= std::min(two, four)) return launch_wide<BT, 8, 8>(w, B, N, C, stream);
-            if (four <= two) return launch_wide<BT, 4, 8>(w, B, N, C, stream);
-            return launch_wide<BT, 2, 4>(w, B, N, C, stream);
+        constexpr bool CODES = BT == SPMM_I8;
+        const int64_t small = us(2, 2, CODES ? 7 : 8), two = us(8, 4, CODES ? 32 : 41), four = us(8, 8, CODES ? 50 : 74), eight = us(16, 8, CODES ? 92 : 124);
+        if (std::min({two, four, eight}) < small) {
+            if (eight <= std::min(two, four)) return launch_wide<BT, 8, 8>(w, B, B_scales, N, C, stream);
+            if (four <= two) return launch_wide<BT, 4, 8>(w, B, B_scales, N, C, stream);
+            return launch_wide<BT, 2, 4>(w, B, B_scales, N, C, stream);
         }
     }
     return launch_many<BT, 2, 2, 8>(w, B, B_scales, N, C, stream);

@@ -81,13 +81,13 @@ def test_whole_numbers_are_exact_in_every_shape_of_workgroup(type, group, M, K):
             check_product(M, K, N, group, type, "features", N + group + 1, whole=True)
 
 
-@pytest.mark.parametrize("type", ["float16", "bfloat16"])
+@pytest.mark.parametrize("type", ["float16", "bfloat16", "int8"])
 @pytest.mark.parametrize("group,zeros", [(32, True), (32, False), (64, True), (64, False), (128, True), (128, False)])
 @pytest.mark.parametrize("N", [2040, 1001, 500])
 def test_whole_numbers_are_exact_in_prompts(type, group, zeros, N):
     """Teams of eight, four and two waves (the token counts); fewer blocks of columns than teams, as many, and more."""
     for n, K in enumerate((100, 390, 650, 1300)):
-        check_product(4090 - 16 * n, K, N, group, type, ("tokens", "features")[n % 2], N + group, whole=True, zeros=zeros)
+        check_product(4090 - 16 * n, K, N, group, type, "features" if n % 2 and type != "int8" else "tokens", N + group, whole=True, zeros=zeros)
 
 
 @pytest.mark.parametrize("type", FLOATS + ("int8",))
