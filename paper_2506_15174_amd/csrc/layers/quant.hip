@@ -318,7 +318,8 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
         for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0, 0, 0, 0};
     asked now, next;
     // B of AHEAD tiles of tokens is on its way while one is multiplied: what the registers hold
-    constexpr int ROOM = BT == SPMM_F32 ? 2 : BT == SPMM_I8 ? 8 : 4, AHEAD = ROOM < NT ? ROOM : NT;
+    constexpr int AHEAD = 2;
+    static_assert(NT % AHEAD == 0);
     u32x4 x[AHEAD][LOADS];
     if (first < last) {
         ask(first, now);
