@@ -470,6 +470,7 @@ template <int BT, int SHARE, int NT, int STEPS, bool ZEROS> __global__ __launch_
     for (int b = first; b < last; ++b) {
         const int round = b - first;
         // This wave's share of the block is there (and what it asked for besides), then the team's; all of them have read the block before.
+        // (The wait ends: a workgroup's waves are all on the compute unit, have as many blocks as their team, and say that they arrived before they wait.)
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __hip_atomic_store(&arrived[wave], round + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         if (b + 1 < last) ask(b + 1, next);
