@@ -80,7 +80,7 @@ spmm_status_t spmm_quant_workspace(const spmm_quant_t *plan, const spmm_tensor_t
  *            one token a row (feature_stride 1, else SPMM_ERR_UNSUPPORTED)
  *   B_scales DEVICE  float[N] where B is SPMM_I8; else not looked at
  *   N        columns of B and C, 1 .. 2^31 - 1
- *   C        M x N, SPMM_F32, SPMM_F16 or SPMM_BF16; every element is overwritten; must not overlap B
+ *   C        M x N, SPMM_F32, SPMM_F16 or SPMM_BF16; every element is overwritten; must not overlap B and B_scales
  *   workspace DEVICE, 16-byte aligned, of spmm_quant_workspace bytes or more (else SPMM_ERR_INVALID_ARG); its
  *            content before the call does not matter
  * Sums are held in 32 bits: weights enter as whole numbers (code - zero), a sum of up to 128 of them, or of a group

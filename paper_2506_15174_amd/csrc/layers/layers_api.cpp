@@ -353,7 +353,8 @@ spmm_status_t spmm_quant_execute(const spmm_quant_t *plan, const spmm_tensor_t *
     if (b.type == SPMM_I8 && (!B_scales || (uintptr_t)B_scales % 4 != 0)) return SPMM_ERR_INVALID_ARG;
     if (w.M == 0) return SPMM_OK;
     if ((st = seen(*C, w.M, N, &c)) != SPMM_OK) return st;
-    if (meet(span_of(b, w.K, N), span_of(c, w.M, N))) return SPMM_ERR_INVALID_ARG;
+    const span scales = {b.type == SPMM_I8 ? reinterpret_cast<const char *>(B_scales) : nullptr, reinterpret_cast<const char *>(B_scales + N)}, to = span_of(c, w.M, N);
+    if (meet(span_of(b, w.K, N), to) || meet(scales, to)) return SPMM_ERR_INVALID_ARG;
     if (!room(workspace, workspace_bytes, quant_workspace(w, b, N))) return SPMM_ERR_INVALID_ARG;
     return status_of(quant_execute(w, b, b.type == SPMM_I8 ? B_scales : nullptr, N, c, static_cast<char *>(workspace), static_cast<hipStream_t>(stream)));
 }

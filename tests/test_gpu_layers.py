@@ -580,6 +580,16 @@ def test_what_the_product_refuses():
         plan.execute(B)
 
 
+def test_the_product_refuses_an_output_over_its_scales():
+    plan, _ = plan_of(6, 10, 32, 1)
+    q, memory = torch.ones((4, 10), dtype=torch.int8, device="cuda").t(), torch.ones(64, device="cuda")
+    for at in (0, 20, 23):
+        with pytest.raises(spmm.SpmmError) as err:
+            plan.execute(q, C=memory[:24].view(6, 4), scales=memory[at:at + 4])
+        assert err.value.status == spmm.binding.SPMM_ERR_INVALID_ARG
+    assert plan.execute(q, C=memory[:24].view(6, 4), scales=memory[24:28]).isfinite().all()
+
+
 def test_what_norm_and_gate_refuse():
     x, w = torch.ones((10, 4), device="cuda"), torch.ones(10, device="cuda")
     for bad in (x.cpu(), x.double(), x.to(torch.int8), x[0], torch.ones((20, 8), device="cuda")[::2, ::2], x[:, :1].expand(10, 4), x[:0], x[:, :0]):
