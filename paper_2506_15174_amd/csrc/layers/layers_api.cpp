@@ -19,6 +19,7 @@ using namespace layers;
 
 struct spmm_quant {
     quant_matrix w = {};
+    int64_t group = 0;  // the caller's; w.group is what the kernels divide by
     int device = -1;
     char *memory = nullptr;
     int64_t bytes = 0;
@@ -143,6 +144,9 @@ spmm_status_t create(spmm_quant_t **plan, int64_t M, int64_t K, int64_t group, c
     if (M > MOST_ROWS || K > MOST_COLS || (group != 32 && group != 64 && group % BLOCK_COLS != 0)) return SPMM_ERR_UNSUPPORTED;
     std::unique_ptr<spmm_quant> p(new spmm_quant);
     quant_matrix &w = p->w;
+    p->group = group;
+    // A group of K columns or more is one whatever its size: the kernels divide by group / 128 in 32 bits, which the least such multiple fits (K is at most 2^30).
+    if (group > BLOCK_COLS) group = std::min(group, up_to(std::max<int64_t>(K, 1), BLOCK_COLS));
     w.M = M, w.K = K, w.group = group;
     w.tiles = (int32_t)parts_of(M, TILE_ROWS), w.blocks = (int32_t)parts_of(K, BLOCK_COLS), w.groups = (int32_t)parts_of(K, group);
     w.span_groups = group < BLOCK_COLS ? (int32_t)(BLOCK_COLS / group) : 1, w.spans = group < BLOCK_COLS ? w.blocks : w.groups;
@@ -322,7 +326,7 @@ spmm_status_t spmm_quant_describe(const spmm_quant_t *plan, int64_t *M, int64_t 
     if (!plan) return SPMM_ERR_INVALID_ARG;
     if (M) *M = plan->w.M;
     if (K) *K = plan->w.K;
-    if (group) *group = plan->w.group;
+    if (group) *group = plan->group;
     if (device_bytes) *device_bytes = plan->bytes;
     return SPMM_OK;
 }
