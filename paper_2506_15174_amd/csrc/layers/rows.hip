@@ -49,7 +49,8 @@ struct token_factors {
         factor = norm ? 1.0f / sqrtf(square / (float)a.features + a.eps) : 1.0f;
         up = most < 0x1p-100f ? 0x1p100f : 1.0f;
         steps = most > 0.0f && most < __builtin_inff() ? 127.0f / (most * up) : 0.0f;
-        scale = most < __builtin_inff() ? most * factor / 127.0f : __builtin_nanf("");
+        // (f is infinite where all of a token's squares vanish and eps is 0)
+        scale = most == 0.0f ? 0.0f : most < __builtin_inff() ? most * factor / 127.0f : __builtin_nanf("");
     }
     __device__ int8_t code(float p) const { return steps == 0.0f ? (int8_t)0 : (int8_t)rintf(p * up * steps); }
 };
