@@ -279,13 +279,17 @@ struct column_tiles {
 // (128 bytes of a row side by side; a thread asks for AT_ONCE rows before it looks at the first)
 constexpr int TILE_THREADS = 256, MOST_SIDE_BITS = 3, PIECE_ROWS = 64, AT_ONCE = 4;
 
+// The first token of a tile `wide` tokens across: the tiles side by side go along the first and the third axis (a launch has less than 2^32 threads along one).
+__device__ inline int64_t first_token(int wide) { return ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * wide; }
+
 template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THREADS) void column_stats_kernel(rows_args a, column_tiles tiles)
 {
     typedef typename element<TYPE>::type E;
     constexpr int U = COLUMN_UNIT<TYPE>;
     __shared__ float squares[4][U << MOST_SIDE_BITS], mosts[4][U << MOST_SIDE_BITS];
     const int side = 1 << tiles.side_bits, col = threadIdx.x & (side - 1), row = threadIdx.x >> tiles.side_bits, step = TILE_THREADS >> tiles.side_bits;
-    const int64_t n0 = (int64_t)blockIdx.x * side * U, n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
+    const int64_t n0 = first_token(side * U), n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
+    if (n0 >= a.tokens) return;
     const int wide = (int)min((int64_t)U, max((int64_t)0, a.tokens - n));
     float square[U], most[U];
 #pragma unroll
@@ -315,7 +319,7 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
 #pragma unroll
     for (int j = 0; j < U; ++j) reduce_lanes<NORM, CODES>(square[j], most[j], side);
     const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) < side) {
+    if ((int)(threadIdx.x & 63) < side) {
 #pragma unroll
         for (int j = 0; j < U; ++j) squares[wave][col * U + j] = square[j], mosts[wave][col * U + j] = most[j];
     }
@@ -334,7 +338,8 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
     __shared__ float sums[2][TILE_THREADS], factors[2][MOST_TOKENS];
     extern __shared__ int8_t turned[];  // codes: [token][rows of a piece + 4]
     const int side = 1 << tiles.side_bits, col = threadIdx.x & (side - 1), row = threadIdx.x >> tiles.side_bits, step = TILE_THREADS >> tiles.side_bits, tokens = side * U;
-    const int64_t n0 = (int64_t)blockIdx.x * tokens, n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
+    const int64_t n0 = first_token(tokens), n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
+    if (n0 >= a.tokens) return;
     const int wide = (int)min((int64_t)U, max((int64_t)0, a.tokens - n));
     // The statistics of this tile's tokens: TILE_THREADS / tokens threads each (tokens is at most TILE_THREADS).
     {
@@ -479,7 +484,7 @@ template <bool NORM, bool CODES, int TYPE> hipError_t launch(const rows_args &a,
         if (cols > 1) return at_once(std::integral_constant<int, 16 / COLUMN_UNIT<TYPE>>());
         column_tiles tiles = tiles_of(K, N, COLUMN_UNIT<TYPE>);
         tiles.partial = reinterpret_cast<float *>(workspace);
-        const dim3 grid((unsigned)tiles.across, (unsigned)((K + tiles.rows - 1) / tiles.rows));
+        const dim3 across = grid_of(tiles.across), grid(across.x, (unsigned)((K + tiles.rows - 1) / tiles.rows), across.y);
         const hipError_t e = launch_kernel(column_stats_kernel<NORM, CODES, TYPE>, grid, TILE_THREADS, 0, stream, a, tiles);
         if (e != hipSuccess) return e;
         const int step = TILE_THREADS >> tiles.side_bits, piece = step > PIECE_ROWS ? step : PIECE_ROWS;

@@ -34,3 +34,40 @@ def test_codes_of_a_token_of_zeros_without_eps(type, K, N, order):
         assert (n.scales == 0).all() and (n.out == 0).all()
     g = spmm.gate(x, x, dtype=torch.int8)
     assert g.scales[0] == 0 and (g.out[:, 0] == 0).all() and (g.scales[1:] > 0).all()
+
+
+# ---- sizes at which a launch takes a second axis ----------------------------------------------------------------
+
+@pytest.mark.parametrize("type,N", [("float32", 2 ** 29 + 77), ("bfloat16", 2 ** 30 + 77)])
+def test_more_tokens_by_features_than_one_axis_of_a_launch_has(type, N):
+    """2^24 tiles side by side: windows of tokens are as from a call on the window alone, which goes in one launch, and the rest is written.
+
+    The statistics of the two need not have the same bits: one of the two squares may be added in one rounding with its product (t_0^2 + t_1^2 as a multiply-add) or in two.  Each
+    side's factor has at most two roundings in the sum, one in the mean and one with eps, all four halved by the root, then one in the root and one in the quotient: 4 half
+    steps.  A scale has two more, its product with P and the division by 127, and a value of the output two, its products with t and the weight: 6 on each side, 12 between them, and twice the output's own."""
+    near = dict(rtol=12 * 2.0 ** -24 * 1.01, atol=0)
+    a, w = torch.empty((2, N), dtype=TYPES[type], device="cuda"), torch.tensor([1.5, -0.75], device="cuda")
+    for k in range(2):
+        a[k].uniform_(0.5, 2.0)
+    y = spmm.norm(a, w, dtype=torch.int8)
+    windows = [0, 2 ** 25 - 700, 2 ** 26 - 700, N // 2 - 333, N - 2000]
+    for n in windows:
+        z = spmm.norm(a[:, n:n + 2000], w, dtype=torch.int8)
+        assert torch.equal(y.out[:, n:n + 2000], z.out) and torch.allclose(y.scales[n:n + 2000].double(), z.scales.double(), **near)
+    assert y.scales.min() > 0 and y.scales.max() < 1
+    for n in range(0, N, 2 ** 27):
+        assert (y.out[:, n:n + 2 ** 27].abs().amax(0) == 127).all()
+    del y, z
+    y = spmm.norm(a, w)
+    for n in windows:
+        z = spmm.norm(a[:, n:n + 2000], w)
+        assert torch.allclose(y.out[:, n:n + 2000].double(), z.out.double(), rtol=(12 * 2.0 ** -24 + (2 * HALF_STEP[type] if type != "float32" else 0)) * 1.01, atol=0)
+    # r lies in 1/2 .. 2: no value of the output is 0
+    for n in range(0, N, 2 ** 27):
+        assert (y.out[0, n:n + 2 ** 27] > 0.3).all() and (y.out[1, n:n + 2 ** 27] < -0.1).all()
+    del y
+    y = spmm.gate(a, act="relu", dtype=torch.int8)
+    for n in windows:
+        z = spmm.gate(a[:, n:n + 2000], act="relu", dtype=torch.int8)
+        assert torch.equal(y.out[:, n:n + 2000], z.out) and torch.equal(y.scales[n:n + 2000], z.scales)
+    assert y.scales.min() > 0

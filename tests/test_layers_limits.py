@@ -27,3 +27,27 @@ def run(program, what):
 
 def test_groups_of_any_size(program):
     run(program, "groups")
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    """The launches' host code, linked with stand-ins for the HIP runtime (the kernels' own code is left out)."""
+    made = tmp_path_factory.mktemp("launches")
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    objects = []
+    for name in ("quant", "rows"):
+        objects.append(str(made / (name + ".o")))
+        subprocess.run([os.path.join(rocm, "bin", "hipcc"), "--offload-arch=gfx950", "--offload-host-only", "-O1", "-fPIC", "-std=c++17", "-w", "-I", CSRC, "-c", os.path.join(CSRC, "layers", name + ".hip"),
+                        "-o", objects[-1]], check=True)
+    exe = str(made / "launches")
+    subprocess.run(["g++", "-O1", "-g", "-std=c++17", "-D__HIP_PLATFORM_AMD__=1", "-I", CSRC, "-I", os.path.join(rocm, "include"), os.path.join(HERE, "layers_launches_on_stand_ins.cpp"),
+                    os.path.join(CSRC, "layers", "layers_api.cpp")] + objects + ["-Wl,--unresolved-symbols=ignore-all", "-pthread", "-o", exe], check=True)
+    return exe
+
+
+def test_launches_of_norm_and_gate_are_within_limits(launches):
+    run(launches, "rows")
+
+
+def test_launches_of_the_product_are_within_limits(launches):
+    run(launches, "products")
