@@ -129,6 +129,8 @@ def quant_plan_create(M, K, codes, scales, zeros=None, group=128):
     multiple of 128.  Arrays are numpy's or torch's.
     """
     M, K, group = int(M), int(K), int(group)
+    if max(abs(M), abs(K), abs(group)) >= 2 ** 63:   # (they would reach the library cut off, and the arrays no longer be those of its sizes)
+        raise ValueError("M, K and group are 64-bit numbers")
     lib = load()
     groups = -(-K // group) if group > 0 else 0
     if M >= 0 and K >= 0:

@@ -29,6 +29,13 @@ def test_groups_of_any_size(program):
     run(program, "groups")
 
 
+@pytest.mark.parametrize("M,K,group", [(6, 300, 2 ** 64 + 128), (6, 300, 2 ** 63), (6, 300, -2 ** 64 + 128), (-2 ** 64 + 6, 300, 128), (6, -2 ** 64 + 300, 128), (2 ** 64 + 6, 300, 128), (6, 2 ** 64 + 300, 128)])
+def test_sizes_of_more_than_64_bits(M, K, group):
+    """Cut off to 64 bits they would be those of larger arrays."""
+    with pytest.raises(ValueError):
+        spmm.quant_plan_create(M, K, np.zeros((6, 150), np.uint8), np.ones((6, 1 if group > 0 else 0), np.float32), group=group)
+
+
 @pytest.fixture(scope="module")
 def launches(tmp_path_factory):
     """The launches' host code, linked with stand-ins for the HIP runtime (the kernels' own code is left out)."""
