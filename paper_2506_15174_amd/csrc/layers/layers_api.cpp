@@ -8,9 +8,11 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 #include <memory>
 #include <new>
 #include <thread>
+#include <utility>
 #include <vector>
 
 #include "layers.h"
@@ -79,19 +81,18 @@ bool meet(const span &a, const span &b) { return a.begin && b.begin && a.begin <
 
 bool same(const tensor &a, const tensor &b) { return a.data == b.data && a.ld == b.ld && a.by_token == b.by_token; }
 
-// One order for two tensors that share it: where one of them has a single row or column, the other's.  False where they differ.
-bool one_order(tensor *a, const tensor &b, int64_t features, int64_t tokens)
+// Whether tensors that share an order have one.  A column without gaps (of one token) is also features of one token each: where another one has gaps, all are seen
+// as that.  (One feature has been seen as a row a token.)
+bool one_order(std::initializer_list<tensor *> tensors, int64_t tokens)
 {
-    if (a->by_token == b.by_token) return true;
-    if (tokens == 1 && a->by_token && a->ld == features) {  // a column without gaps: also features of one token
-        *a = {a->data, 1, a->type, false};
+    bool features = false, rows = false;
+    for (const tensor *t : tensors) (t->by_token ? rows : features) = true;
+    if (tokens == 1 && features) {
+        for (tensor *t : tensors)
+            if (t->by_token) *t = {t->data, 1, t->type, false};
         return true;
     }
-    if (features == 1 && !a->by_token && a->ld == tokens) {
-        *a = {a->data, 1, a->type, true};
-        return true;
-    }
-    return false;
+    return !(features && rows);
 }
 
 // Codes and scales of the tiles [t0, t1) (layers.h).
@@ -221,8 +222,8 @@ bool room(const void *workspace, size_t bytes, int64_t needed)
     return needed == 0 || (workspace && (uintptr_t)workspace % 16 == 0 && bytes >= (size_t)needed);
 }
 
-// What norm and gate have in common: input, its optional companion, output and scales.
-spmm_status_t seen_rows(int64_t features, int64_t tokens, const spmm_tensor_t &x, const spmm_tensor_t &y, const spmm_tensor_t &out, float *scales, rows_args *a)
+// What norm and gate have in common: input, its optional companion, output and scales; `total` is the norm's.
+spmm_status_t seen_rows(int64_t features, int64_t tokens, const spmm_tensor_t &x, const spmm_tensor_t &y, const spmm_tensor_t &total, const spmm_tensor_t &out, float *scales, rows_args *a)
 {
     if (!extents(features, tokens)) return SPMM_ERR_INVALID_ARG;
     a->features = features, a->tokens = tokens;
@@ -230,39 +231,31 @@ spmm_status_t seen_rows(int64_t features, int64_t tokens, const spmm_tensor_t &x
     if (st != SPMM_OK) return st;
     if (x.type == SPMM_I8) return SPMM_ERR_INVALID_ARG;
     if ((st = seen(out, features, tokens, &a->out)) != SPMM_OK) return st;
-    if (y.data) {
-        if (y.type != x.type) return SPMM_ERR_INVALID_ARG;
-        if ((st = seen(y, features, tokens, &a->y)) != SPMM_OK) return st;
-        if (!one_order(&a->y, a->x, features, tokens) && !one_order(&a->x, a->y, features, tokens)) return SPMM_ERR_UNSUPPORTED;
+    for (auto [given, to] : {std::pair{&y, &a->y}, std::pair{&total, &a->total}}) {
+        if (!given->data) continue;
+        if (given->type != x.type) return SPMM_ERR_INVALID_ARG;
+        if ((st = seen(*given, features, tokens, to)) != SPMM_OK) return st;
     }
     if (out.type == SPMM_I8) {
         if (!scales || (uintptr_t)scales % 4 != 0) return SPMM_ERR_INVALID_ARG;
         a->scales = scales;
-        if (!a->out.by_token) {
-            if (features != 1 || a->out.ld != tokens) return SPMM_ERR_UNSUPPORTED;
-            a->out = {a->out.data, 1, SPMM_I8, true};
-        }
-    } else if (!one_order(&a->out, a->x, features, tokens)) {
-        if (!one_order(&a->x, a->out, features, tokens) || (y.data && !one_order(&a->y, a->out, features, tokens))) return SPMM_ERR_UNSUPPORTED;
+        if (!a->out.by_token) return SPMM_ERR_UNSUPPORTED;
     }
-    return SPMM_OK;
+    // (what is not there goes with x)
+    tensor *const others[] = {out.type == SPMM_I8 ? &a->x : &a->out, y.data ? &a->y : &a->x, total.data ? &a->total : &a->x};
+    return one_order({&a->x, others[0], others[1], others[2]}, tokens) ? SPMM_OK : SPMM_ERR_UNSUPPORTED;
 }
 
 spmm_status_t seen_norm(int64_t K, int64_t N, const spmm_norm_t *args, rows_args *a)
 {
     if (!args) return SPMM_ERR_INVALID_ARG;
     *a = {};
-    spmm_status_t st = seen_rows(K, N, args->x, args->residual, args->out, args->scales, a);
+    const spmm_status_t st = seen_rows(K, N, args->x, args->residual, args->total, args->out, args->scales, a);
     if (st != SPMM_OK) return st;
     if (!args->weight || args->weight_type < SPMM_F32 || args->weight_type > SPMM_BF16 || (uintptr_t)args->weight % (uintptr_t)size_of(args->weight_type) != 0 ||
         !(args->eps >= 0.0f))
         return SPMM_ERR_INVALID_ARG;
     a->weight = static_cast<const char *>(args->weight), a->weight_type = args->weight_type, a->eps = args->eps;
-    if (args->total.data) {
-        if (args->total.type != args->x.type) return SPMM_ERR_INVALID_ARG;
-        if ((st = seen(args->total, K, N, &a->total)) != SPMM_OK) return st;
-        if (!one_order(&a->total, a->x, K, N)) return SPMM_ERR_UNSUPPORTED;
-    }
     const span total = span_of(a->total, K, N), out = span_of(a->out, K, N), x = span_of(a->x, K, N), y = span_of(a->y, K, N);
     const span weight = {a->weight, a->weight + K * size_of(a->weight_type)}, scales = {reinterpret_cast<char *>(a->scales), reinterpret_cast<char *>(a->scales + N)};
     if (meet(out, x) || meet(out, y) || meet(out, total) || meet(out, weight) || meet(out, scales) || meet(total, weight) || meet(total, scales) || meet(scales, x) ||
@@ -275,7 +268,7 @@ spmm_status_t seen_gate(int64_t F, int64_t N, const spmm_gate_t *args, rows_args
 {
     if (!args) return SPMM_ERR_INVALID_ARG;
     *a = {};
-    const spmm_status_t st = seen_rows(F, N, args->a, args->b, args->out, args->scales, a);
+    const spmm_status_t st = seen_rows(F, N, args->a, args->b, {}, args->out, args->scales, a);
     if (st != SPMM_OK) return st;
     if (args->act < SPMM_ACT_SILU || args->act > SPMM_ACT_RELU) return SPMM_ERR_INVALID_ARG;
     a->act = args->act;
@@ -298,10 +291,7 @@ spmm_status_t seen_operand(const quant_matrix &w, const spmm_tensor_t *B, int64_
     *b = {nullptr, 1, B->type, true};
     if (w.K == 0) return SPMM_OK;
     const spmm_status_t st = seen(*B, w.K, N, b);
-    if (st != SPMM_OK || b->type != SPMM_I8 || b->by_token) return st;
-    if (w.K != 1 || b->ld != N) return SPMM_ERR_UNSUPPORTED;
-    *b = {b->data, 1, SPMM_I8, true};
-    return SPMM_OK;
+    return st == SPMM_OK && b->type == SPMM_I8 && !b->by_token ? SPMM_ERR_UNSUPPORTED : st;
 }
 
 }  // namespace

@@ -27,10 +27,46 @@ static void groups()
     }
 }
 
+// One token: every tensor with gaps or without, in any combination.  A column without gaps (strides 1 and anything) and a column of a wider matrix (strides
+// LD and 1, as features of one token each) have one order.
+static void one_token()
+{
+    float weight[16] = {0};
+    for (int gaps = 0; gaps < 16; ++gaps)
+        for (int out_type : {SPMM_F32, SPMM_BF16, SPMM_I8})
+            for (bool residual : {false, true})
+                for (bool total : {false, true}) {
+                    auto column = [&](void *data, int n, int type) { return gaps >> n & 1 ? spmm_tensor_t{data, 5 + n, 1, type} : spmm_tensor_t{data, 1, 3, type}; };
+                    spmm_norm_t a = {};
+                    a.x = column(B, 0, SPMM_F32), a.out = column(C, 3, out_type), a.weight = weight, a.scales = S;
+                    if (residual) a.residual = column(D, 1, SPMM_F32);
+                    if (total) a.total = column(B + 4096, 2, SPMM_F32);
+                    spmm_gate_t g = {};
+                    g.a = a.x, g.b = a.residual, g.out = a.out, g.scales = S;
+                    const bool codes = out_type == SPMM_I8;
+                    for (bool norm : {true, false}) {
+                        memset((void *)&last_rows, 0, sizeof last_rows);
+                        const spmm_status_t st = norm ? spmm_norm(10, 1, &a, nullptr, 0, nullptr) : spmm_gate(10, 1, &g, nullptr, 0, nullptr);
+                        if (codes && gaps >> 3 & 1) {   // codes lie one token a row
+                            CHECK(st == SPMM_ERR_UNSUPPORTED);
+                            continue;
+                        }
+                        CHECK(st == SPMM_OK);
+                        const layers::tensor *seen[] = {&last_rows.x, &last_rows.y, &last_rows.total, &last_rows.out};
+                        for (int n = 0; n < 4; ++n) {
+                            if (!seen[n]->data || (n == 3 && codes)) continue;
+                            CHECK(seen[n]->by_token == last_rows.x.by_token && (seen[n]->by_token ? !(gaps >> n & 1) : seen[n]->ld == (gaps >> n & 1 ? 5 + n : 1)));
+                        }
+                        CHECK((last_rows.y.data != nullptr) == residual && (last_rows.total.data != nullptr) == (norm && total) && (!codes || last_rows.out.by_token));
+                    }
+                }
+}
+
 int main(int argc, char **argv)
 {
     const char *what = argc > 1 ? argv[1] : "";
     if (!strcmp(what, "groups")) groups();
+    else if (!strcmp(what, "one token")) one_token();
     else return 2;
     printf("ok\n");
     return 0;

@@ -71,3 +71,27 @@ def test_more_tokens_by_features_than_one_axis_of_a_launch_has(type, N):
         z = spmm.gate(a[:, n:n + 2000], act="relu", dtype=torch.int8)
         assert torch.equal(y.out[:, n:n + 2000], z.out) and torch.equal(y.scales[n:n + 2000], z.scales)
     assert y.scales.min() > 0
+
+
+# ---- one token ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("K", [1, 7, 300, 5000])
+def test_one_token_in_columns_with_gaps_and_without(K):
+    """Any of the tensors may be a column of a wider matrix, the sum too.  With gaps the squares are added up in another order: a chain of at most K / 16 + 256 roundings on each side,
+    halved by the root, then eight single ones."""
+    near = dict(rtol=2 * ((K / 16 + 256) / 2 + 8) * 2.0 ** -24, atol=0)
+    rng = np.random.default_rng(K)
+    values = [torch.from_numpy(rng.standard_normal((K, 1))).float().cuda() for _ in range(2)]
+    w = torch.ones(K, device="cuda")
+    want = spmm.norm(values[0], w, residual=values[1])
+    codes = spmm.norm(values[0], w, residual=values[1], dtype=torch.int8)
+    for gaps in range(16):
+        def column(n, value=None):
+            t = torch.full((K, 4), 7.0, device="cuda")[:, 1:2] if gaps >> n & 1 else torch.full((K, 1), 7.0, device="cuda")
+            return t if value is None else t.copy_(value)
+        x, r = column(0, values[0]), column(1, values[1])
+        y = spmm.norm(x, w, residual=r, total=column(2), out=column(3))
+        assert torch.equal(y.total, want.total) and torch.allclose(y.out, want.out, **near)
+        z = spmm.norm(x, w, residual=r, total=column(2), dtype=torch.int8)
+        assert torch.equal(z.total, want.total) and torch.equal(z.out, codes.out) and torch.allclose(z.scales, codes.scales, **near)
+        assert torch.equal(spmm.gate(x, r, out=column(3)).out, spmm.gate(values[0], values[1]).out)
