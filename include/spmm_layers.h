@@ -27,7 +27,9 @@ enum { SPMM_F32 = 0, SPMM_F16 = 1, SPMM_BF16 = 2, SPMM_I8 = 3 };
  * (strides in elements).  One of the two strides is 1:
  *   token_stride 1    one row of memory a feature, as B and C of spmm_execute; feature_stride >= tokens
  *   feature_stride 1  one row of memory a token; token_stride >= features
- * A stride along an extent of one element is not looked at.  data is aligned to its element; it may be NULL where
+ * A stride along an extent of one element is not looked at.  Two tensors overlap where an element of one lies in one of
+ * the other: rows of memory may lie between those of another tensor that are as far apart (in bytes; rows that are not as
+ * far apart, of which some lie between the other's first and last, count as overlapping).  data is aligned to its element; it may be NULL where
  * the tensor is optional (the other fields are then not looked at) and where it has no element.
  */
 typedef struct {

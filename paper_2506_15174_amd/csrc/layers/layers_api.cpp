@@ -66,18 +66,36 @@ spmm_status_t seen(const spmm_tensor_t &t, int64_t features, int64_t tokens, ten
     return out->ld > INT64_MAX / 8 / rows ? SPMM_ERR_INVALID_ARG : SPMM_OK;
 }
 
+// Rows of `row` bytes, `pitch` bytes apart (0: one row).
 struct span {
     const char *begin, *end;
+    int64_t row, pitch;
 };
+
+span span_of(const void *vector, int64_t bytes)
+{
+    const char *begin = static_cast<const char *>(vector);
+    return {begin, begin ? begin + bytes : nullptr, bytes, 0};
+}
 
 span span_of(const tensor &t, int64_t features, int64_t tokens)
 {
-    if (!t.data) return {nullptr, nullptr};
-    const int64_t rows = t.by_token ? tokens : features, row = t.by_token ? features : tokens;
-    return {t.data, t.data + ((rows - 1) * t.ld + row) * size_of(t.type)};
+    if (!t.data) return {};
+    const int64_t rows = t.by_token ? tokens : features, row = (t.by_token ? features : tokens) * size_of(t.type), pitch = t.ld * size_of(t.type);
+    const int64_t bytes = (rows - 1) * pitch + row;
+    if (pitch == row || rows == 1) return span_of(t.data, bytes);
+    return {t.data, t.data + bytes, row, pitch};
 }
 
-bool meet(const span &a, const span &b) { return a.begin && b.begin && a.begin < b.end && b.begin < a.end; }
+// Whether two of them share memory.  Rows of one pitch may lie between each other; of two pitches it is not looked at whether they do.
+bool meet(const span &a, const span &b)
+{
+    if (!a.begin || !b.begin || a.begin >= b.end || b.begin >= a.end) return false;
+    const int64_t pitch = a.pitch ? a.pitch : b.pitch;
+    if (pitch == 0 || (b.pitch != 0 && b.pitch != pitch)) return true;
+    const int64_t d = ((b.begin - a.begin) % pitch + pitch) % pitch;  // from a row of a to the next start of one of b
+    return d < a.row || d + b.row > pitch;
+}
 
 bool same(const tensor &a, const tensor &b) { return a.data == b.data && a.ld == b.ld && a.by_token == b.by_token; }
 
@@ -257,7 +275,7 @@ spmm_status_t seen_norm(int64_t K, int64_t N, const spmm_norm_t *args, rows_args
         return SPMM_ERR_INVALID_ARG;
     a->weight = static_cast<const char *>(args->weight), a->weight_type = args->weight_type, a->eps = args->eps;
     const span total = span_of(a->total, K, N), out = span_of(a->out, K, N), x = span_of(a->x, K, N), y = span_of(a->y, K, N);
-    const span weight = {a->weight, a->weight + K * size_of(a->weight_type)}, scales = {reinterpret_cast<char *>(a->scales), reinterpret_cast<char *>(a->scales + N)};
+    const span weight = span_of(a->weight, K * size_of(a->weight_type)), scales = span_of(a->scales, N * 4);
     if (meet(out, x) || meet(out, y) || meet(out, total) || meet(out, weight) || meet(out, scales) || meet(total, weight) || meet(total, scales) || meet(scales, x) ||
         meet(scales, y) || meet(scales, weight) || (meet(total, x) && !same(a->total, a->x)) || (meet(total, y) && !same(a->total, a->y)))
         return SPMM_ERR_INVALID_ARG;
@@ -273,7 +291,7 @@ spmm_status_t seen_gate(int64_t F, int64_t N, const spmm_gate_t *args, rows_args
     if (args->act < SPMM_ACT_SILU || args->act > SPMM_ACT_RELU) return SPMM_ERR_INVALID_ARG;
     a->act = args->act;
     const span out = span_of(a->out, F, N), x = span_of(a->x, F, N), y = span_of(a->y, F, N);
-    const span scales = {reinterpret_cast<char *>(a->scales), reinterpret_cast<char *>(a->scales + N)};
+    const span scales = span_of(a->scales, N * 4);
     if (meet(out, x) || meet(out, y) || meet(out, scales) || meet(scales, x) || meet(scales, y)) return SPMM_ERR_INVALID_ARG;
     return SPMM_OK;
 }
@@ -347,7 +365,7 @@ spmm_status_t spmm_quant_execute(const spmm_quant_t *plan, const spmm_tensor_t *
     if (b.type == SPMM_I8 && (!B_scales || (uintptr_t)B_scales % 4 != 0)) return SPMM_ERR_INVALID_ARG;
     if (w.M == 0) return SPMM_OK;
     if ((st = seen(*C, w.M, N, &c)) != SPMM_OK) return st;
-    const span scales = {b.type == SPMM_I8 ? reinterpret_cast<const char *>(B_scales) : nullptr, reinterpret_cast<const char *>(B_scales + N)}, to = span_of(c, w.M, N);
+    const span scales = span_of(b.type == SPMM_I8 ? B_scales : nullptr, N * 4), to = span_of(c, w.M, N);
     if (meet(span_of(b, w.K, N), to) || meet(scales, to)) return SPMM_ERR_INVALID_ARG;
     if (!room(workspace, workspace_bytes, quant_workspace(w, b, N))) return SPMM_ERR_INVALID_ARG;
     return status_of(quant_execute(w, b, b.type == SPMM_I8 ? B_scales : nullptr, N, c, static_cast<char *>(workspace), static_cast<hipStream_t>(stream)));

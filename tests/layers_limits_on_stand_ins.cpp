@@ -62,11 +62,75 @@ static void one_token()
                 }
 }
 
+// Outputs between the rows of inputs, against a look at every byte.  Two tensors in one piece of memory, of all places and sizes that fit.
+static void between_rows()
+{
+    float weight[64] = {0}, scales[64] = {0};
+    uint8_t codes[64] = {0};
+    spmm_quant_t *plan[8] = {};
+    for (int M = 1; M <= 5; M += 2) CHECK(spmm_quant_create(&plan[M], M, 3, 32, codes, weight, nullptr) == SPMM_OK);
+    long taken = 0, refused = 0, apart_and_refused = 0;
+    for (int order = 0; order < 2; ++order)
+        for (int N = 1; N <= 4; ++N)
+            for (int M = 1; M <= 5; M += 2)
+                for (int ld : {5, 8, 9})
+                    for (int out_ld : {5, 8, 9})
+                        for (int at = 0; at < 80; ++at) {
+                            auto tensor_at = [&](float *data, int pitch) { return order ? spmm_tensor_t{data, 1, pitch, SPMM_F32} : spmm_tensor_t{data, pitch, 1, SPMM_F32}; };
+                            auto bytes_of = [&](const float *data, int features, int pitch) {
+                                std::set<const float *> s;
+                                for (int f = 0; f < features; ++f)
+                                    for (int n = 0; n < N; ++n) s.insert(data + (order ? n * pitch + f : f * pitch + n));
+                                return s;
+                            };
+                            auto share = [](const std::set<const float *> &a, const std::set<const float *> &b) {
+                                for (const float *p : a)
+                                    if (b.count(p)) return true;
+                                return false;
+                            };
+                            float *const in = B + 200, *const out = B + 160 + at;
+                            auto judge = [&](spmm_status_t st, bool overlap, bool one_pitch) {
+                                CHECK(st == (overlap ? SPMM_ERR_INVALID_ARG : SPMM_OK) || (!one_pitch && st == SPMM_ERR_INVALID_ARG));
+                                ++(st == SPMM_OK ? taken : refused);
+                                apart_and_refused += st != SPMM_OK && !overlap;
+                            };
+                            const bool single = order ? N == 1 : false;
+                            // the product: B is 3 x N, C is M x N
+                            const spmm_tensor_t b = tensor_at(in, ld), c = tensor_at(out, out_ld);
+                            judge(spmm_quant_execute(plan[M], &b, nullptr, N, &c, room, 64, nullptr), share(bytes_of(in, 3, ld), bytes_of(out, M, out_ld)), ld == out_ld || single || (M == 1 && !order));
+                            if (M == 3) {
+                                spmm_gate_t g = {};
+                                g.a = b, g.out = c;
+                                judge(spmm_gate(3, N, &g, nullptr, 0, nullptr), share(bytes_of(in, 3, ld), bytes_of(out, 3, out_ld)), ld == out_ld || single);
+                                spmm_norm_t n = {};
+                                n.x = b, n.out = tensor_at(C, 9), n.total = c, n.weight = D;
+                                const bool same = in == out && (ld == out_ld || (order && N == 1));
+                                judge(spmm_norm(3, N, &n, nullptr, 0, nullptr), !same && share(bytes_of(in, 3, ld), bytes_of(out, 3, out_ld)), ld == out_ld || single);
+                                // a vector between the rows
+                                n.total = {}, n.weight = C + 4 + at % 8, n.weight_type = SPMM_F32;
+                                std::set<const float *> vector = {C + 4 + at % 8, C + 5 + at % 8, C + 6 + at % 8};
+                                judge(spmm_norm(3, N, &n, nullptr, 0, nullptr), share(vector, bytes_of(C, 3, 9)), true);
+                            }
+                        }
+    CHECK(taken > 5000 && refused > 5000 && apart_and_refused > 0);
+    // codes and their scales in one piece of memory: rows of 12 bytes, 3 of them codes
+    spmm_gate_t g = {};
+    g.a = {B, 1, 3, SPMM_F32}, g.out = {C, 1, 12, SPMM_I8};
+    g.scales = scales;
+    CHECK(spmm_gate(3, 4, &g, nullptr, 0, nullptr) == SPMM_OK);
+    g.scales = C + 1;   // 16 bytes in a pitch of 12
+    CHECK(spmm_gate(3, 4, &g, nullptr, 0, nullptr) == SPMM_ERR_INVALID_ARG);
+    g.out.token_stride = 32;
+    CHECK(spmm_gate(3, 4, &g, nullptr, 0, nullptr) == SPMM_OK);
+    for (spmm_quant_t *p : plan) CHECK(spmm_quant_destroy(p) == SPMM_OK);
+}
+
 int main(int argc, char **argv)
 {
     const char *what = argc > 1 ? argv[1] : "";
     if (!strcmp(what, "groups")) groups();
     else if (!strcmp(what, "one token")) one_token();
+    else if (!strcmp(what, "between rows")) between_rows();
     else return 2;
     printf("ok\n");
     return 0;

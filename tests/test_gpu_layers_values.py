@@ -95,3 +95,34 @@ def test_one_token_in_columns_with_gaps_and_without(K):
         z = spmm.norm(x, w, residual=r, total=column(2), dtype=torch.int8)
         assert torch.equal(z.total, want.total) and torch.equal(z.out, codes.out) and torch.allclose(z.scales, codes.scales, **near)
         assert torch.equal(spmm.gate(x, r, out=column(3)).out, spmm.gate(values[0], values[1]).out)
+
+
+# ---- outputs between the rows of inputs ----------------------------------------------------------------------------
+
+def beside(type, order, sizes, N):
+    """Tensors of sizes[i] features x N in one piece of memory, side by side in its rows (order "tokens") or rows of memory one below the other, every second one used."""
+    if order == "tokens":
+        memory = torch.full((N, sum(sizes) + 3), 7.0, dtype=TYPES[type], device="cuda")
+        at = [sum(sizes[:i]) for i in range(len(sizes))]
+        return [memory[:, a:a + s].t() for a, s in zip(at, sizes)], memory[:, sum(sizes):]
+    rows = max(sizes)
+    memory = torch.full((rows, len(sizes) * N + 3), 7.0, dtype=TYPES[type], device="cuda")
+    return [memory[:s, i * N:(i + 1) * N] for i, s in enumerate(sizes)], memory[:, len(sizes) * N:]
+
+
+@pytest.mark.parametrize("type", FLOATS)
+@pytest.mark.parametrize("order", ["tokens", "features"])
+@pytest.mark.parametrize("M,K,N", [(50, 300, 3), (50, 300, 20), (300, 500, 150), (2100, 300, 600)])
+def test_outputs_between_the_rows_of_inputs(type, order, M, K, N):
+    """B and C, and x, residual, sum and output, in one piece of memory; what lies between stays."""
+    codes, scales, zeros, _ = weights(M, K, 64, K + N)
+    plan = spmm.quant_plan_create(M, K, codes, scales, zeros, group=64)
+    a, r = (torch.from_numpy(np.random.default_rng(s).standard_normal((K, N))).to(TYPES[type]).cuda() for s in (1, 2))
+    w = torch.ones(K, device="cuda")
+    (B, C), rest = beside(type, order, (K, M), N)
+    assert torch.equal(plan.execute(B.copy_(a), C), plan.execute(a if order == "features" else a.t().contiguous().t())) and torch.equal(B, a) and (rest == 7).all()
+    (x, y, t, o), rest = beside(type, order, (K,) * 4, N)
+    got, want = spmm.norm(x.copy_(a), w, residual=y.copy_(r), total=t, out=o), spmm.norm(x.clone(), w, residual=y.clone())
+    assert torch.equal(got.out, want.out) and torch.equal(got.total, want.total) and torch.equal(x, a) and torch.equal(y, r) and (rest == 7).all()
+    o.fill_(7)
+    assert torch.equal(spmm.gate(x, y, out=o).out, spmm.gate(x.clone(), y.clone()).out) and torch.equal(x, a) and torch.equal(y, r) and torch.equal(t, want.total) and (rest == 7).all()

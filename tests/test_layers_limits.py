@@ -33,6 +33,10 @@ def test_one_token_in_columns_with_gaps_and_without(program):
     run(program, "one token")
 
 
+def test_outputs_between_the_rows_of_inputs(program):
+    run(program, "between rows")
+
+
 @pytest.mark.parametrize("M,K,group", [(6, 300, 2 ** 64 + 128), (6, 300, 2 ** 63), (6, 300, -2 ** 64 + 128), (-2 ** 64 + 6, 300, 128), (6, -2 ** 64 + 300, 128), (2 ** 64 + 6, 300, 128), (6, 2 ** 64 + 300, 128)])
 def test_sizes_of_more_than_64_bits(M, K, group):
     """Cut off to 64 bits they would be those of larger arrays."""
