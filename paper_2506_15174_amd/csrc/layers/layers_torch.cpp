@@ -63,6 +63,14 @@ const at::Tensor *tensor_of(PyObject *o, const char *name)
     return &THPVariable_Unpack(o);
 }
 
+// torch keeps the imaginary part of a conjugate as memory of the other sign and a mark.
+void unmarked(const at::Tensor &t, const char *name)
+{
+    if (!t.is_neg()) return;
+    PyErr_Format(PyExc_ValueError, "%s is a view whose negation is still to be made (resolve_neg() makes it)", name);
+    throw raised();
+}
+
 // A 2-D device tensor of the given types (a mask over SPMM_*) as the library sees it.
 spmm_tensor_t seen(const at::Tensor &t, const char *name, unsigned types)
 {
@@ -77,6 +85,7 @@ spmm_tensor_t seen(const at::Tensor &t, const char *name, unsigned types)
         PyErr_Format(PyExc_ValueError, "%s must have a stride of 1 along its features or its tokens, and no two elements in one place", name);
         throw raised();
     }
+    unmarked(t, name);
     return {t.data_ptr(), s0, s1, type};
 }
 
@@ -101,6 +110,7 @@ void vector_of(const at::Tensor &t, const char *name, int64_t n, bool floats_onl
         PyErr_Format(PyExc_ValueError, "%s must be a contiguous %s device tensor of %lld elements", name, floats_only ? "float32" : "float32, float16 or bfloat16", (long long)n);
         throw raised();
     }
+    unmarked(t, name);
 }
 
 // The device has to be the current one, as plans and streams are bound to theirs.

@@ -126,3 +126,26 @@ def test_outputs_between_the_rows_of_inputs(type, order, M, K, N):
     assert torch.equal(got.out, want.out) and torch.equal(got.total, want.total) and torch.equal(x, a) and torch.equal(y, r) and (rest == 7).all()
     o.fill_(7)
     assert torch.equal(spmm.gate(x, y, out=o).out, spmm.gate(x.clone(), y.clone()).out) and torch.equal(x, a) and torch.equal(y, r) and torch.equal(t, want.total) and (rest == 7).all()
+
+
+# ---- views that torch has not made yet -----------------------------------------------------------------------------
+
+def test_views_whose_negation_is_still_to_be_made():
+    """Their memory holds the other sign: refused wherever a tensor goes in or out, taken once they are made."""
+    codes, scales, _, W = weights(6, 10, 32, 1, zeros=False)
+    plan = spmm.quant_plan_create(6, 10, codes, scales, group=32)
+    part = torch.randn((10, 1, 2), device="cuda")
+    lazy = torch.view_as_complex(part).conj().imag
+    assert lazy.is_neg() and lazy.shape == (10, 1)
+    x, w = torch.randn((10, 1), device="cuda"), torch.ones(10, device="cuda")
+    out = torch.view_as_complex(torch.zeros((6, 1, 2), device="cuda")).conj().imag
+    one = torch.view_as_complex(torch.ones((1, 2), device="cuda")).conj().imag
+    q = torch.ones((10, 1), dtype=torch.int8, device="cuda")
+    for call in (lambda: plan.execute(lazy), lambda: plan.execute(x, out), lambda: plan.execute(q, scales=one), lambda: spmm.norm(lazy, w), lambda: spmm.norm(x, w, residual=lazy),
+                 lambda: spmm.norm(x, w, total=lazy), lambda: spmm.norm(x, w, out=lazy), lambda: spmm.norm(x[:1], one), lambda: spmm.norm(x, w, dtype=torch.int8, scales=one),
+                 lambda: spmm.gate(lazy), lambda: spmm.gate(x, lazy), lambda: spmm.gate(x, out=lazy), lambda: spmm.gate(x, dtype=torch.int8, scales=one)):
+        with pytest.raises(ValueError, match="negation"):
+            call()
+    made = lazy.resolve_neg()
+    assert torch.equal(made, -part[:, :, 1]) and torch.equal(plan.execute(made), plan.execute(-part[:, :, 1]))
+    assert torch.equal(spmm.norm(made, w).out, spmm.norm((-part[:, :, 1]).contiguous(), w).out)
