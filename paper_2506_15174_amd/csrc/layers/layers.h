@@ -56,6 +56,7 @@ struct rows_args {
     int32_t weight_type;
     float eps;
     int32_t act;
+    double per_feature;  // 1 / features
 };
 
 int64_t rows_workspace(const rows_args &a, bool norm);

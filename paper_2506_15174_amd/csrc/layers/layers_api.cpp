@@ -244,7 +244,7 @@ bool room(const void *workspace, size_t bytes, int64_t needed)
 spmm_status_t seen_rows(int64_t features, int64_t tokens, const spmm_tensor_t &x, const spmm_tensor_t &y, const spmm_tensor_t &total, const spmm_tensor_t &out, float *scales, rows_args *a)
 {
     if (!extents(features, tokens)) return SPMM_ERR_INVALID_ARG;
-    a->features = features, a->tokens = tokens;
+    a->features = features, a->tokens = tokens, a->per_feature = 1.0 / (double)features;
     spmm_status_t st = seen(x, features, tokens, &a->x);
     if (st != SPMM_OK) return st;
     if (x.type == SPMM_I8) return SPMM_ERR_INVALID_ARG;

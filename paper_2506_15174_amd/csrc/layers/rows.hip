@@ -5,6 +5,8 @@
 //   gate                       p = act(a) b;  f = 1
 //   out = p f (norm: t f w), or code = rint(p (127 / max |p|)), scale = max |p| f / 127
 //
+// Squares are added up in fp32 by a thread, over up to 32 of them, and by the lanes of a wave, from there on in 64 bits: what a few waves or tiles leave costs nothing to add up, and the mean is right to
+// its rounding (in fp32 throughout, 15 waves' sums could vanish beside one).
 // Codes do not wait for f: they depend on p alone, so one look at the token gives both statistics.  All of it is bound by
 // memory, or by the latency of one launch: elements are read once and held in registers between the statistics
 // and the output where registers hold them.  With the residual's addition, us (of which a launch is 2.4): one token of 4096 in bf16 3.3; 2048 tokens of 8192 in bf16 28, 4.8 TB/s, in codes 27;
@@ -44,9 +46,9 @@ struct token_factors {
     float factor;     // f
     float up, steps;  // code = rint(p * up * steps); up keeps 127 / max |p| finite for the smallest values
     float scale;
-    __device__ token_factors(bool norm, float square, float most, const rows_args &a)
+    __device__ token_factors(bool norm, double square, float most, const rows_args &a)
     {
-        factor = norm ? 1.0f / sqrtf(square / (float)a.features + a.eps) : 1.0f;
+        factor = norm ? 1.0f / sqrtf((float)(square * a.per_feature + a.eps)) : 1.0f;
         up = most < 0x1p-100f ? 0x1p100f : 1.0f;
         steps = most > 0.0f && most < __builtin_inff() ? 127.0f / (most * up) : 0.0f;
         // (f is infinite where all of a token's squares vanish and eps is 0)
@@ -116,14 +118,15 @@ template <bool NORM, bool CODES, int TYPE, int T, int R, int TOKENS> __global__ 
         }
     }
     reduce_lanes<NORM, CODES>(square, most, 1);
+    double sum = square;
     if constexpr (WAVES > 1) {
         if ((t & 63) == 0) squares[t / 64] = square, mosts[t / 64] = most;
         __syncthreads();
-        square = squares[0], most = mosts[0];
+        sum = squares[0], most = mosts[0];
 #pragma unroll
-        for (int wave = 1; wave < WAVES; ++wave) square += squares[wave], most = fmaxf(most, mosts[wave]);
+        for (int wave = 1; wave < WAVES; ++wave) sum += squares[wave], most = fmaxf(most, mosts[wave]);
     }
-    const token_factors f(NORM, square, most, a);
+    const token_factors f(NORM, sum, most, a);
     if (CODES && t == 0) a.scales[n] = f.scale;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -148,7 +151,8 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(1024) vo
     const int t = threadIdx.x;
     const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (n >= a.tokens) return;
-    float square = 0.0f, most = 0.0f;
+    double of_thread = 0.0;
+    float most = 0.0f;
     for (int64_t k = t * UNIT; k < a.features; k += 1024 * UNIT) {
         const int there = (int)min((int64_t)UNIT, a.features - k);
         float v[UNIT], w[UNIT];
@@ -156,18 +160,22 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(1024) vo
         if constexpr (NORM)
             if (a.total.data) store_row<E>(a.total.data, n * a.total.ld + k, there, v);
         if constexpr (NORM && CODES) load_row_as(a.weight, k, there, a.weight_type, w);
+        float square = 0.0f;
 #pragma unroll
         for (int j = 0; j < UNIT; ++j) {
             if constexpr (NORM) square += v[j] * v[j];
             if constexpr (CODES) most = larger(most, NORM ? v[j] * w[j] : v[j]);
         }
+        of_thread += square;
     }
+    float square = (float)of_thread;
     reduce_lanes<NORM, CODES>(square, most, 1);
     if ((t & 63) == 0) squares[t / 64] = square, mosts[t / 64] = most;
     __syncthreads();
-    square = squares[0], most = mosts[0];
-    for (int wave = 1; wave < 16; ++wave) square += squares[wave], most = fmaxf(most, mosts[wave]);
-    const token_factors f(NORM, square, most, a);
+    double sum = squares[0];
+    most = mosts[0];
+    for (int wave = 1; wave < 16; ++wave) sum += squares[wave], most = fmaxf(most, mosts[wave]);
+    const token_factors f(NORM, sum, most, a);
     if (CODES && t == 0) a.scales[n] = f.scale;
     for (int64_t k = t * UNIT; k < a.features; k += 1024 * UNIT) {
         const int there = (int)min((int64_t)UNIT, a.features - k);
@@ -229,7 +237,8 @@ template <bool NORM, bool CODES, int TYPE, int COLS, int HELD> __global__ __laun
     }
     __syncthreads();
     if (threadIdx.x < TOKENS && n0 + threadIdx.x < a.tokens) {  // a thread a token
-        float s = squares[0][threadIdx.x], m = mosts[0][threadIdx.x];
+        double s = squares[0][threadIdx.x];
+        float m = mosts[0][threadIdx.x];
         for (int w = 1; w < WAVES; ++w) s += squares[w][threadIdx.x], m = fmaxf(m, mosts[w][threadIdx.x]);
         const token_factors f(NORM, s, m, a);
         if (CODES) a.scales[n0 + threadIdx.x] = f.scale;
@@ -291,11 +300,14 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
     const int64_t n0 = first_token(side * U), n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
     if (n0 >= a.tokens) return;
     const int wide = (int)min((int64_t)U, max((int64_t)0, a.tokens - n));
+    double of_thread[U];
     float square[U], most[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j) square[j] = most[j] = 0.0f;
+    for (int j = 0; j < U; ++j) of_thread[j] = 0.0, most[j] = 0.0f;
     for (int64_t k = k0 + row; k < k1; k += AT_ONCE * step) {
         float v[AT_ONCE][U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) square[j] = 0.0f;
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
             const int64_t at = k + i * step;
@@ -315,7 +327,13 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
                 if constexpr (CODES) most[j] = larger(most[j], v[i][j] * w[0]);
             }
         }
+        if constexpr (NORM) {
+#pragma unroll
+            for (int j = 0; j < U; ++j) of_thread[j] += square[j];
+        }
     }
+#pragma unroll
+    for (int j = 0; j < U; ++j) square[j] = (float)of_thread[j];
 #pragma unroll
     for (int j = 0; j < U; ++j) reduce_lanes<NORM, CODES>(square[j], most[j], side);
     const int wave = threadIdx.x >> 6;
@@ -327,7 +345,7 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
     for (int t = threadIdx.x; t < side * U; t += TILE_THREADS) {
         if (n0 + t >= a.tokens) continue;
         float *to = tiles.partial + (int64_t)blockIdx.y * 2 * a.tokens + n0 + t;
-        if constexpr (NORM) to[0] = squares[0][t] + squares[1][t] + squares[2][t] + squares[3][t];
+        if constexpr (NORM) to[0] = (float)((double)squares[0][t] + squares[1][t] + squares[2][t] + squares[3][t]);
         if constexpr (CODES) to[a.tokens] = fmaxf(fmaxf(mosts[0][t], mosts[1][t]), fmaxf(mosts[2][t], mosts[3][t]));
     }
 }
@@ -335,7 +353,8 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
 template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THREADS) void column_apply_kernel(rows_args a, column_tiles tiles)
 {
     constexpr int U = COLUMN_UNIT<TYPE>, MOST_TOKENS = U << MOST_SIDE_BITS;
-    __shared__ float sums[2][TILE_THREADS], factors[2][MOST_TOKENS];
+    __shared__ double sums[TILE_THREADS];
+    __shared__ float mosts[TILE_THREADS], factors[2][MOST_TOKENS];
     extern __shared__ int8_t turned[];  // codes: [token][rows of a piece + 4]
     const int side = 1 << tiles.side_bits, col = threadIdx.x & (side - 1), row = threadIdx.x >> tiles.side_bits, step = TILE_THREADS >> tiles.side_bits, tokens = side * U;
     const int64_t n0 = first_token(tokens), n = n0 + col * U, k0 = (int64_t)blockIdx.y * tiles.rows, k1 = min(k0 + tiles.rows, a.features);
@@ -344,7 +363,8 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
     // The statistics of this tile's tokens: TILE_THREADS / tokens threads each (tokens is at most TILE_THREADS).
     {
         const int t = threadIdx.x & (tokens - 1), token_bits = tiles.side_bits + (U == 4 ? 2 : 3), part = threadIdx.x >> token_bits, parts = TILE_THREADS >> token_bits;
-        float s = 0.0f, m = 0.0f;
+        double s = 0.0;
+        float m = 0.0f;
         if (n0 + t < a.tokens) {
             for (int c = part; c < (int)gridDim.y; c += parts) {
                 const float *from = tiles.partial + (int64_t)c * 2 * a.tokens + n0 + t;
@@ -352,10 +372,10 @@ template <bool NORM, bool CODES, int TYPE> __global__ __launch_bounds__(TILE_THR
                 if constexpr (CODES) m = fmaxf(m, from[a.tokens]);
             }
         }
-        sums[0][threadIdx.x] = s, sums[1][threadIdx.x] = m;
+        sums[threadIdx.x] = s, mosts[threadIdx.x] = m;
         __syncthreads();
         if (part == 0) {
-            for (int p = 1; p < parts; ++p) s += sums[0][p * tokens + t], m = fmaxf(m, sums[1][p * tokens + t]);
+            for (int p = 1; p < parts; ++p) s += sums[p * tokens + t], m = fmaxf(m, mosts[p * tokens + t]);
             const token_factors f(NORM, s, m, a);
             if (CODES && blockIdx.y == 0 && n0 + t < a.tokens) a.scales[n0 + t] = f.scale;
             factors[0][t] = CODES ? f.up : f.factor;

@@ -149,3 +149,27 @@ def test_views_whose_negation_is_still_to_be_made():
     made = lazy.resolve_neg()
     assert torch.equal(made, -part[:, :, 1]) and torch.equal(plan.execute(made), plan.execute(-part[:, :, 1]))
     assert torch.equal(spmm.norm(made, w).out, spmm.norm((-part[:, :, 1]).contiguous(), w).out)
+
+
+# ---- the norm's statistics -----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("type", FLOATS)
+@pytest.mark.parametrize("K,N,order,step", [(8000, 3, "tokens", 512), (16000, 3, "tokens", 512), (30000, 3, "tokens", 512), (70000, 2, "tokens", 512), (8000, 600, "tokens", 512),
+                                            (1024, 128, "features", 16), (1024, 128, "features", 32), (4096, 6, "features", 64), (5000, 270, "features", 128), (8192, 270, "features", 128)])
+def test_what_waves_leave_is_not_lost_beside_a_large_square(type, K, N, order, step):
+    """One square of 2^24 and single ones in other waves' or tiles' shares, 2^24 + 15 where there are 16 waves: in fp32 none of the ones would move the sum.
+
+    The sum is exact then.  The mean is rounded (a half step, halved by the root), the root, the quotient, the product with t: 3.5 half steps of fp32; a scale has the division by
+    127 besides."""
+    x = torch.zeros((K, N), dtype=torch.float64)
+    ones = torch.arange(step, min(K, 16 * step if order == "tokens" or step < 100 else K), step)
+    for n in range(N):
+        x[ones[: max(1, len(ones) - n % 3)], n] = 1.0
+    x[0] = 4096.0
+    d = placed(x.numpy(), type, order)
+    w = torch.ones(K, device="cuda")
+    f = 1 / np.sqrt((x.numpy() ** 2).mean(0))
+    y = spmm.norm(d, w, 0.0, dtype=torch.float32)
+    assert (np.abs(as64(y.out) - x.numpy() * f) <= 3.5 * 2.0 ** -24 * 1.01 * x.numpy() * f).all()
+    z = spmm.norm(d, w, 0.0, dtype=torch.int8)
+    assert (np.abs(as64(z.scales) - 4096 * f / 127) <= 4.5 * 2.0 ** -24 * 1.01 * 4096 * f / 127).all()
