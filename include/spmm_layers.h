@@ -141,7 +141,9 @@ typedef struct {
 } spmm_gate_t;
 
 /*
- * Gated activation: out = act(a) * b, in fp32 (8-bit output: p = act(a) * b, f = 1).  F, N and the workspace as for
+ * Gated activation: out = act(a) * b, in fp32 (8-bit output: p = act(a) * b, f = 1).  silu and gelu are right to 2^-20 of
+ * their value, u = a and u = 2 sqrt(2 / pi) (a + 0.044715 a^3) taken as they come out in fp32 and values below 2^-119 counting as 0 or not;
+ * where out is not SPMM_F32, before its rounding, to (2 |u| + 16) 2^-24.  F, N and the workspace as for
  * spmm_norm.  out must not overlap a, b and scales.
  */
 spmm_status_t spmm_gate_workspace(int64_t F, int64_t N, const spmm_gate_t *args, size_t *bytes);

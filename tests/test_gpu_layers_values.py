@@ -173,3 +173,39 @@ def test_what_waves_leave_is_not_lost_beside_a_large_square(type, K, N, order, s
     assert (np.abs(as64(y.out) - x.numpy() * f) <= 3.5 * 2.0 ** -24 * 1.01 * x.numpy() * f).all()
     z = spmm.norm(d, w, 0.0, dtype=torch.int8)
     assert (np.abs(as64(z.scales) - 4096 * f / 127) <= 4.5 * 2.0 ** -24 * 1.01 * 4096 * f / 127).all()
+
+
+# ---- the gate's activation -----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("order", ["tokens", "features"])
+def test_silu_is_as_exact_for_large_arguments(order):
+    """In half steps of fp32 (2^-24), relative: the exponential's instruction 2, what its argument's rounding left 1 (and less than 0.1 for all that is neglected of it), the product with x 1, the sum
+    1 + e 1, the reciprocal's instruction 2, the quotient 1, the product with b 1: 9.1.  Below 2^-126 an exponential may count as 0."""
+    F, N = 4096, 16
+    rng = np.random.default_rng(11)
+    a = placed(rng.uniform(-100, 100, (F, N)) * rng.uniform(0, 1, (1, N)), "float32", order)
+    b = placed(rng.uniform(0.5, 2, (F, N)), "float32", order)
+    a64, b64 = as64(a), as64(b)
+    want = a64 * np.exp(np.minimum(a64, 0)) / (1 + np.exp(-np.abs(a64)))
+    for second in (None, b):
+        w = want if second is None else want * b64
+        got = as64(spmm.gate(a, second).out)
+        assert (np.abs(got - w) <= 9.1 * 2.0 ** -24 * np.abs(w) + 2.0 ** -126 * 128 * 2).all()
+    y = spmm.gate(a, b, dtype=torch.int8)
+    most = np.abs(want * b64).max(0)
+    # P, and its division by 127
+    assert (np.abs(as64(y.scales) - most / 127) <= 10.1 * 2.0 ** -24 * most / 127).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_small_results_of_the_gate(act):
+    """x exp(x) at -86, where 1 + exp(86) would have a reciprocal below the normal numbers.  The instruction for the exponential gives 0 for results below 2^-126, as exp(-87.5) = 1.0e-38 is (2^-126 is
+    1.18e-38): there the result is off by all of itself, |x| exp(x), which is less than |x| 2^-126."""
+    x = np.array([[-80.0], [-86.0], [-87.5]]) if act == "silu" else np.array([[-9.0], [-10.0], [-10.3]])
+    got = as64(spmm.gate(placed(x, "float32", "features"), act=act).out)
+    x = as64(placed(x, "float32", "features", device="cpu"))
+    u = x if act == "silu" else 2 * np.sqrt(2 / np.pi) * (x + 0.044715 * x ** 3)
+    want = x * np.exp(u) / (1 + np.exp(u))
+    # gelu's u has four roundings of its own, of at most |u| 2^-24 each (its constants' among them), and an error of u is one of the result
+    rel = 9.1 * 2.0 ** -24 + (0 if act == "silu" else 5 * np.abs(u) * 2.0 ** -24)
+    assert (np.abs(got - want) <= rel * np.abs(want) + np.where(np.exp(u) < 2.0 ** -126, np.abs(x) * 2.0 ** -126, 0)).all()
