@@ -112,6 +112,15 @@ __device__ inline uint32_t apart(uint32_t v)
     return v;
 }
 
+// What lanes of a wave have written to LDS is there for its other lanes: the hardware takes a wave's accesses to LDS in order, so this only keeps the compiler from changing it.  (Accesses to
+// other memory may pass.)
+__device__ inline void lanes_in_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 template <int BT> __device__ inline operands<BT> operands_of(const raw<BT> &x)
 {
     operands<BT> o;
@@ -622,6 +631,7 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
         operands<BT> o[NT][4];
         if constexpr (STAGED && !decltype(tail)::value) {
             char *const mine = staged + wave * (PARTS<BT> * 16 * PITCH);
+            lanes_in_lds();  // (the lanes' reads of the block before)
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
                 char *const to = mine + (p * ROWS_AT_ONCE + lane / ROW_LANES) * PITCH + lane % ROW_LANES * (16 / SIZE * PART_SIZE);
@@ -639,6 +649,7 @@ template <int BT, bool BY_TOKEN, int PER_GROUP, int RT, int NT, int KWAVES, int 
                     *reinterpret_cast<u32x4 *>(to) = a.piece[p];
                 }
             }
+            lanes_in_lds();
             const char *const from = mine + r * PITCH + 8 * q * PART_SIZE;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
