@@ -117,7 +117,8 @@ typedef struct {
 /*
  * Root-mean-square norm over the features of every token, with the residual's addition:
  *   t = x + residual in fp32, rounded to x's type;  r = 1 / sqrt(mean_k t^2 + eps), in fp32;  out = t * r * weight
- * (8-bit output: p = t * weight, f = r).  Squares of values beyond 2^63 overflow, as they do in fp32 arithmetic.
+ * (8-bit output: p = t * weight, f = r).  Squares of values beyond 2^63 overflow and those of values
+ * below 2^-75 are 0, as in fp32 arithmetic.
  *   K  features, 1 .. 2^31 - 1;  N  tokens, 1 .. 2^31 - 1
  *   workspace  DEVICE, 16-byte aligned, of spmm_norm_workspace bytes or more (0: may be NULL)
  * out and total must not overlap each other, nor x, residual, weight and scales but as said above.

@@ -8,7 +8,7 @@
 // needs one scale a group.
 //
 // Up to 16 tokens, and somewhat more on short rows, go in one launch (direct_kernel): bound by a launch's few memory accesses, then by the weights' bytes.  More take two: pack_kernel
-// lays B out as the instructions take it, then many_kernel, bound by B's way through the vector L1, or, on prompts of all but fp32, wide_kernel, bound by the matrix cores and by
+// lays B out as the instructions take it, then many_kernel, half of whose time B's way through the vector L1 takes, or, on prompts of all but fp32, wide_kernel, bound by the matrix cores and by
 // the instructions that make operands of weights.
 #include <algorithm>
 #include <hip/hip_runtime.h>
@@ -105,7 +105,8 @@ template <> struct operands<SPMM_I8> {
 };
 
 // A value in a register of its own.  Without this the compiler (ROCm 7.2) gave operands made of a wide load's words the load's own registers and wrote the first
-// before it read the last: v18 = perm(v39, v38), then v20 = perm(v19, v18), where v18 to v21 held the words 4 to 7.
+// before it read the last: v18 = perm(v39, v38), then v20 = perm(v19, v18), where v18 to v21 held the words 4 to 7.  (That was an earlier form of the callers; the assembly of the
+// present ones has no such place with it or without.  It costs some moves, 2 % of all instructions here; the cause is not known.)
 __device__ inline uint32_t apart(uint32_t v)
 {
     asm("" : "+v"(v));
@@ -269,7 +270,8 @@ template <int BT> constexpr float WEIGHT_UNIT = BT == SPMM_F32 || BT == SPMM_BF1
 //
 // A wave has RT tiles of rows and NT tiles of tokens, a workgroup KWAVES such waves that share K; their sums meet in LDS.  Weights become operands once a block and
 // are used for all of its tokens, B (laid out by pack_kernel) comes a tile of tokens at a time, the next one while one is multiplied.  With the layout of B: 4096 x 4096, 128 tokens
-// in bf16 14.8 us, 291 TF; 8192 x 8192, 512 in fp32 227 us, 303 TF (three products of bf16 for each).
+// in bf16 14.0 us, 307 TF; 8192 x 8192, 512 in fp32 220 us, 312 TF (three products of bf16 for each).  8192 x 8192, 128 in bf16, 37 us: of 94 k clocks the address unit before the vector L1 is busy 50 k, vector
+// instructions issue for 44 k, matrix instructions take 16 k; waves wait for memory half of their time.
 
 template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ __launch_bounds__(64 * KWAVES) void many_kernel(quant_matrix W, const char *B, const float *B_scales, int64_t N,
                                                                                                                           tensor C)
@@ -422,8 +424,9 @@ template <int BT, int NT, int RT, int KWAVES, int STEPS, bool ZEROS> __global__ 
 // way there while the block before is multiplied.  A team waits for its own waves only: with a barrier for the workgroup 8192 x 8192, 512 tokens, took 105 us, without 89 (teams of two;
 // a second block on its way, with which waves of a team may be a block apart, gained nothing).  Weights are made operands by each wave for itself, 13 instructions for a tile of rows and
 // 32 columns, which matrix instructions share with NT tiles of tokens: 128 tokens a wave instead of 64 take 81 us and 83, in teams of eight 142 and 150 on 1024 (LDS does not hold
-// them for teams of two).  Two waves a SIMD issue an instruction of that kind in 4.8 clocks, and what both kinds take adds up rather than overlaps, also where the program interleaves them.
-// 8192 x 8192 in bf16, with 6 us to lay out B for 512 tokens: 512 81 us, 850 TF; 4096 546, 1006 TF; in codes 512 60 us, 1150 TOPS, 2048 197 us, 1400 TOPS.
+// them for teams of two).  8192 x 8192, 512 in bf16: of 175 k clocks a SIMD's matrix instructions take 65 k (37 %), 15 k other vector instructions of 4 clocks 60 k; waves wait for memory or LDS 31 % of
+// their time and to issue 31 %.  Putting the two kinds in turn by the program gained nothing (with 64 tokens a wave).
+// 8192 x 8192 in bf16, with 6 us to lay out B for 512 tokens: 512 79 us, 870 TF; 4096 544, 1010 TF; in codes 512 57 us, 1210 TOPS, 2048 198 us, 1390 TOPS.
 
 constexpr int WIDE_LDS = 128 * 1024;
 
@@ -566,8 +569,8 @@ template <int V> using constant = std::integral_constant<int, V>;
 // ---- in one launch ---------------------------------------------------------------------------------------------
 //
 // A product of few tokens is over in the time of a few memory accesses, of which a launch is two or three: every wave reads its columns of
-// B as it reads its weights and makes operands of them itself.  In bf16, one token: 4096 x 4096 4.3 us, 2.1 TB/s of weights and all; 8192 x 8192 10.4 us, 3.4 TB/s; 16384 x 16384
-// 36 us, 3.9 TB/s, where a large copy reaches 5.1.  Lanes of tokens that do not exist read the last one's (an access the
+// B as it reads its weights and makes operands of them itself.  In bf16, one token, weights from memory: 4096 x 4096 4.9 us, 1.8 TB/s of weights and scales; 8192 x 8192 10.9 us, 3.3 TB/s; 16384 x 16384
+// 37 us, 3.9 TB/s, where a large copy reaches 5.1 (from the Infinity Cache 3.5 and 9.1 us).  Lanes of tokens that do not exist read the last one's (an access the
 // wave makes anyway); their results are not stored.  Weights, scales and B of AHEAD blocks are asked for before the first is used.
 //   PER_GROUP  steps of 32 columns behind which a group's sum is full (4, 2 or 1)
 //   RT, NT     tiles of rows and of tokens of a wave

@@ -9,9 +9,9 @@
 // its rounding (in fp32 throughout, 15 waves' sums could vanish beside one).
 // Codes do not wait for f: they depend on p alone, so one look at the token gives both statistics.  All of it is bound by
 // memory, or by the latency of one launch: elements are read once and held in registers between the statistics
-// and the output where registers hold them.  With the residual's addition, us (of which a launch is 2.4): one token of 4096 in bf16 3.3; 2048 tokens of 8192 in bf16 28, 4.8 TB/s, in codes 27;
-// where a row of memory is a feature, fp32, 128 tokens of 1024 6.9, 2048 tokens of 4096 47, 2.9 TB/s (3.6 with the sum's second reading).  The gate: 16 tokens of 4096 in f16 2.6; 2048 of
-// 16384 in bf16 37, 5.5 TB/s.
+// and the output where registers hold them.  With the residual's addition, us (of which a launch is 2.4): one token of 4096 in bf16 3.1; 2048 tokens of 8192 in bf16 29, 4.6 TB/s, in codes 30;
+// where a row of memory is a feature, fp32, 128 tokens of 1024 6.7, 2048 tokens of 4096 46, 2.9 TB/s (3.6 with the sum's second reading).  The gate: 16 tokens of 4096 in f16 2.3; 2048 of
+// 16384 in bf16 37, 5.4 TB/s, 2048 of 8192 to codes 21 (by features 50, where values are read and made twice).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
