@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2506_15174_amd as spmm
-from layers_reference import HALF_STEP, SMALLEST, TYPES, act64, as64, codes_of, placed, summed, weights
+from layers_reference import HALF_STEP, TYPES, as64, placed, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -100,7 +100,7 @@ def test_one_token_in_columns_with_gaps_and_without(K):
 # ---- outputs between the rows of inputs ----------------------------------------------------------------------------
 
 def beside(type, order, sizes, N):
-    """Tensors of sizes[i] features x N in one piece of memory, side by side in its rows (order "tokens") or rows of memory one below the other, every second one used."""
+    """Tensors of sizes[i] features x N side by side in the rows of one piece of memory, and what the rows hold behind them."""
     if order == "tokens":
         memory = torch.full((N, sum(sizes) + 3), 7.0, dtype=TYPES[type], device="cuda")
         at = [sum(sizes[:i]) for i in range(len(sizes))]
