@@ -89,7 +89,7 @@ static void between_rows()
                                 return false;
                             };
                             float *const in = B + 200, *const out = B + 160 + at;
-                            auto judge = [&](spmm_status_t st, bool overlap, bool one_pitch) {
+                            auto answered = [&](spmm_status_t st, bool overlap, bool one_pitch) {
                                 CHECK(st == (overlap ? SPMM_ERR_INVALID_ARG : SPMM_OK) || (!one_pitch && st == SPMM_ERR_INVALID_ARG));
                                 ++(st == SPMM_OK ? taken : refused);
                                 apart_and_refused += st != SPMM_OK && !overlap;
@@ -97,19 +97,19 @@ static void between_rows()
                             const bool single = order ? N == 1 : false;
                             // the product: B is 3 x N, C is M x N
                             const spmm_tensor_t b = tensor_at(in, ld), c = tensor_at(out, out_ld);
-                            judge(spmm_quant_execute(plan[M], &b, nullptr, N, &c, room, 64, nullptr), share(bytes_of(in, 3, ld), bytes_of(out, M, out_ld)), ld == out_ld || single || (M == 1 && !order));
+                            answered(spmm_quant_execute(plan[M], &b, nullptr, N, &c, room, 64, nullptr), share(bytes_of(in, 3, ld), bytes_of(out, M, out_ld)), ld == out_ld || single || (M == 1 && !order));
                             if (M == 3) {
                                 spmm_gate_t g = {};
                                 g.a = b, g.out = c;
-                                judge(spmm_gate(3, N, &g, nullptr, 0, nullptr), share(bytes_of(in, 3, ld), bytes_of(out, 3, out_ld)), ld == out_ld || single);
+                                answered(spmm_gate(3, N, &g, nullptr, 0, nullptr), share(bytes_of(in, 3, ld), bytes_of(out, 3, out_ld)), ld == out_ld || single);
                                 spmm_norm_t n = {};
                                 n.x = b, n.out = tensor_at(C, 9), n.total = c, n.weight = D;
                                 const bool same = in == out && (ld == out_ld || (order && N == 1));
-                                judge(spmm_norm(3, N, &n, nullptr, 0, nullptr), !same && share(bytes_of(in, 3, ld), bytes_of(out, 3, out_ld)), ld == out_ld || single);
+                                answered(spmm_norm(3, N, &n, nullptr, 0, nullptr), !same && share(bytes_of(in, 3, ld), bytes_of(out, 3, out_ld)), ld == out_ld || single);
                                 // a vector between the rows
                                 n.total = {}, n.weight = C + 4 + at % 8, n.weight_type = SPMM_F32;
                                 std::set<const float *> vector = {C + 4 + at % 8, C + 5 + at % 8, C + 6 + at % 8};
-                                judge(spmm_norm(3, N, &n, nullptr, 0, nullptr), share(vector, bytes_of(C, 3, 9)), true);
+                                answered(spmm_norm(3, N, &n, nullptr, 0, nullptr), share(vector, bytes_of(C, 3, 9)), true);
                             }
                         }
     CHECK(taken > 5000 && refused > 5000 && apart_and_refused > 0);
